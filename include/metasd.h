@@ -99,6 +99,12 @@ enum metasd_path {
 #define METASD_STATUS_TIMEOUT   8u /* a bounded device-side wait on an asynchronous copy ran out (see wait_poll_limit): the
                                       call still ends, its outputs are undefined, the context stays usable */
 #define METASD_STATUS_BAD_LENGTH 32u /* a registered per-sequence draft length was outside 1 .. k: it was clamped */
+#define METASD_STATUS_BAD_INDEX 64u   /* metasd_verify_probs: a draft_place outside [0, batch); metasd_cache_plan: a pool >= n_pools */
+#define METASD_STATUS_NO_BLOCKS 128u  /* metasd_cache_plan: a pool had too few free blocks; the sequences that went without are
+                                         not planned (their slots are -1) */
+#define METASD_STATUS_TRUNCATED 256u  /* metasd_cache_plan: the step has more than max_tokens entries; the sequences that did not fit
+                                         are not planned */
+#define METASD_STATUS_BAD_STATE 512u  /* a cache's counts are outside their range, or more blocks came back than it has */
 #define METASD_STATUS_BAD_POINTER 16u /* the drafter table of a call held a NULL or misaligned entry: its rows are never
                                         read and the outputs of the sequences that played that drafter are meaningless */
 
@@ -284,6 +290,97 @@ int metasd_verify_noalloc(int32_t batch, int32_t k, int32_t vocab, int32_t logit
                           int32_t reward_kind, uint64_t seed, uint32_t sequence_base, uint32_t round,
                           int32_t *accepted_len, int32_t *next_token, float *reward,
                           uint32_t *status_out, void *stream);
+
+/* One verification round from probabilities and given random numbers, for callers that cut their distributions (top-k,
+ * min-p, penalties) or draw their numbers themselves: Algorithm 4's verification loop on p and q as they stand.
+ *
+ *   accept x_j           iff u_accept[b, j] * q_j(x_j) < p_j(x_j)
+ *   next token           the first v whose running sum of w, in token order, is above u_draw[b] * sum(w); w = max(0, p_n - q_n) at
+ *                        the first rejection n (w = p_n where that leaves nothing), w = p at position k_b if all were accepted
+ *   d_tv[b, j]           1/2 sum_v |p_j(v) - q_j(v)|, j < k_b
+ *
+ * The rows need not be normalised: the accept test takes the values as they are, the draw divides by its own sum.  Without d_tv
+ * only the drafted tokens' entries and the row (pair) that the next token is drawn from are read.
+ *
+ *   ctx            NULL: stateless.  Else the round is one of this context's: batch <= max_batch, 1 <= k <= max_draft, vocab as
+ *                  configured; the configured reward (BD: from the d_TV, BE: N_acc / k_b) goes to `reward` and to the bandits, whose
+ *                  next selection metasd_select then returns; status bits go to the context (status is NULL).
+ *   device         CUDA device ordinal of the buffers and of `stream`; of the context where there is one
+ *   k              0 .. 16; 0: a token is drawn from the target's one row, and what belongs to drafts may be NULL
+ *   vocab          V, up to 2^30
+ *   prob_dtype     metasd_dtype of both sides
+ *   target_probs   row j of sequence b starts target_seq_stride * b + target_row_stride * j entries in, j <= k; strides >= 0
+ *   draft_probs    the same for j < k, of sequence draft_place[b] (of b where draft_place is NULL: a permutation, as
+ *                  metasd_cache_plan's `place`, reads the rows in the order in which the drafters left them); NULL: the drafters
+ *                  were certain (a lookup): q is 1 at the drafted token
+ *   draft_tokens   [batch, k]
+ *   draft_len      [batch] drafted tokens per sequence, 0 .. k (with a context 1 .. k, and NULL stands for the lengths of
+ *                  metasd_set_draft_lengths), or NULL: k; others are clamped and flagged.  Nothing behind them is read or written.
+ *   u_accept       [batch, k] fp32, u_draw [batch] fp32: uniforms in [0, 1)
+ *   seed           with a context: key of the randomised policies' arms, as in metasd_verify
+ *   accepted_len   [batch], next_token [batch]
+ *   d_tv           optional [batch, k] fp32
+ *   reward         with a context: [batch] fp32; else NULL
+ *   status         optional, without a context: device uint32 that METASD_STATUS_* bits are OR-ed into
+ *
+ * Defined outcomes: an entry of a drafted token that is NaN, infinite or negative rejects it, a row that holds such an entry has
+ * d_TV 1 and gives token -1, as a row of zeros does (METASD_STATUS_NONFINITE); a drafted token outside the vocabulary is
+ * rejected; a certain drafter's distance to such a token is 1; q(x) = 0 < p(x) is accepted.
+ * Launches kernels only (one; with a context two): may be captured.  Results are the same, bit for bit, in a batch of any size. */
+int metasd_verify_probs(metasd_ctx *ctx, int32_t device, int32_t batch, int32_t k, int32_t vocab, int32_t prob_dtype,
+                        const void *target_probs, int64_t target_seq_stride, int64_t target_row_stride,
+                        const void *draft_probs, int64_t draft_seq_stride, int64_t draft_row_stride,
+                        const int32_t *draft_place, const int32_t *draft_tokens, const int32_t *draft_len,
+                        const float *u_accept, const float *u_draw, uint64_t seed, int32_t *accepted_len,
+                        int32_t *next_token, float *d_tv, float *reward, uint32_t *status, void *stream);
+
+/* The paged caches of the models of a round: the target's, or the drafters' (one pool each).  A drafter that the bandit leaves falls
+ * behind and has to be brought up to date when it is chosen again (the paper's switching cost), so the sequences of a step
+ * add different numbers of entries to different models' caches.  All memory is the caller's; the calls below keep it up to date. */
+#define METASD_MAX_POOLS 32
+typedef struct metasd_cache {
+    int32_t *block_table;   /* [n_pools, max_batch, max_blocks]: the blocks of each sequence, in order; the first `held` count */
+    int32_t *held;          /* [n_pools, max_batch] */
+    int32_t *free_blocks;   /* [n_pools, n_blocks]: a stack of the pool's free blocks; the first free_count count */
+    int32_t *free_count;    /* [n_pools] */
+    void *workspace;        /* metasd_cache_workspace_bytes(max_batch, n_pools) bytes, 16-byte aligned, of this cache alone */
+    uint32_t *status;       /* optional: METASD_STATUS_* bits are OR-ed into it */
+    int32_t n_pools;        /* 1 .. METASD_MAX_POOLS */
+    int32_t max_batch;      /* 1 .. 65535 */
+    int32_t max_blocks;     /* of a sequence */
+    int32_t n_blocks;       /* the most free blocks of a pool */
+    int32_t page_size;      /* entries of a block, any number >= 1 */
+    int32_t device;         /* CUDA device ordinal */
+} metasd_cache;
+
+size_t metasd_cache_workspace_bytes(int32_t max_batch, int32_t n_pools);   /* 0: sizes out of range */
+
+/* Plans a step: sequence b < batch brings the cache of pool[b] from cached to length[b] entries.
+ *
+ *   pool          [batch]: the model the sequence runs on (metasd_select's arms); negative: it takes no part; NULL: pool 0
+ *   cached        entries of sequence b in pool g's cache: cached[g * cached_pool_stride + b]; held * page_size at most
+ *   length        [batch]; where it is not above `cached` nothing is added (and nothing given back)
+ *   order         optional [batch]: the sequences by pool, in sequence order within each; those that take no part at the end
+ *   place         optional [batch]: the inverse, order[place[b]] == b
+ *   pool_start    optional [n_pools + 1]: the first place of each pool, and the first of those that take no part
+ *   token_start   [batch + 1], by place: running sum of the new entries
+ *   slot_map      [max_tokens] int64: block_table[pool][b][position / page_size] * page_size + position % page_size of every
+ *                 new entry; -1: its sequence is not planned (METASD_STATUS_NO_BLOCKS, METASD_STATUS_TRUNCATED)
+ *   position      optional [max_tokens]; sequence: optional [max_tokens], the sequence of every new entry
+ *
+ * Blocks are taken from the end of the pool's free list, sequence after sequence in that order; from the first sequence on for
+ * which too few are left, none of the pool gets any (those that need none are planned).  Behind token_start[batch] the
+ * outputs are left as they were.  A sequence whose lengths do not fit its table (METASD_STATUS_BAD_LENGTH) or whose pool does not
+ * exist (METASD_STATUS_BAD_INDEX) adds nothing.  Launches kernels only; calls on one cache must be stream-ordered. */
+int metasd_cache_plan(const metasd_cache *cache, int32_t batch, const int32_t *pool, const int32_t *cached,
+                      int64_t cached_pool_stride, const int32_t *length, int32_t max_tokens, int32_t *order,
+                      int32_t *place, int32_t *pool_start, int32_t *token_start, int64_t *slot_map,
+                      int32_t *position, int32_t *sequence, void *stream);
+
+/* Gives back the blocks that sequences b < batch hold beyond keep entries (rejected drafts, finished queries), in every pool:
+ * keep[g * keep_pool_stride + b] entries stay (0: nothing; more than are held: all).  The free list grows so that the next plan
+ * takes the blocks in the order (sequence, then position) in which they were held: a release undoes a plan. */
+int metasd_cache_release(const metasd_cache *cache, int32_t batch, const int32_t *keep, int64_t keep_pool_stride, void *stream);
 
 const char *metasd_strerror(int code);
 

@@ -22,6 +22,7 @@ REWARD_BD, REWARD_BE = 0, 1
 PATH_AUTO, PATH_STREAMING, PATH_FUSED = 0, 1, 2
 ROWS_AUTO, ROWS_PLAIN, ROWS_STAGED, ROWS_BULK = 0, 1, 2, 3
 STATUS_NONFINITE, STATUS_TOKEN_OOR, STATUS_Q_ZERO, STATUS_TIMEOUT, STATUS_BAD_POINTER, STATUS_BAD_LENGTH = 1, 2, 4, 8, 16, 32
+STATUS_BAD_INDEX, STATUS_NO_BLOCKS, STATUS_TRUNCATED, STATUS_BAD_STATE = 64, 128, 256, 512
 
 OK, ERR_INVALID_ARGUMENT, ERR_UNSUPPORTED, ERR_CUDA, ERR_NO_MEMORY, ERR_BAD_STATE_BLOB = 0, -1, -2, -3, -4, -5
 
@@ -33,8 +34,10 @@ EXPORTS = (
     "metasd_verify", "metasd_verify_host", "metasd_state_bytes", "metasd_state_export",
     "metasd_state_import", "metasd_last_status", "metasd_kernel_launches", "metasd_resolved_path",
     "metasd_strerror", "metasd_verify_noalloc", "metasd_set_draft_lengths", "metasd_state_validate",
-    "metasd_resolved_row_kernel",
+    "metasd_resolved_row_kernel", "metasd_verify_probs", "metasd_cache_workspace_bytes", "metasd_cache_plan",
+    "metasd_cache_release",
 )
+MAX_POOLS = 32
 
 
 class MetasdConfig(C.Structure):
@@ -55,6 +58,15 @@ class MetasdDiag(C.Structure):
     """Mirror of ``metasd_diag`` (20 bytes)."""
     _fields_ = [("p_x", C.c_float), ("q_x", C.c_float), ("D", C.c_float), ("u", C.c_float),
                 ("accept", C.c_int32)]
+
+
+class MetasdCache(C.Structure):
+    """Mirror of ``metasd_cache``."""
+    _fields_ = [
+        ("block_table", C.c_void_p), ("held", C.c_void_p), ("free_blocks", C.c_void_p), ("free_count", C.c_void_p),
+        ("workspace", C.c_void_p), ("status", C.c_void_p), ("n_pools", C.c_int32), ("max_batch", C.c_int32),
+        ("max_blocks", C.c_int32), ("n_blocks", C.c_int32), ("page_size", C.c_int32), ("device", C.c_int32),
+    ]
 
 
 class MetasdError(RuntimeError):
@@ -101,9 +113,17 @@ def load_library(path: Optional[str] = None):
     lib.metasd_state_validate.argtypes = [C.POINTER(MetasdConfig), vp, C.c_size_t]
     lib.metasd_verify_noalloc.argtypes = [i32, i32, i32, i32, vp, vp, vp, C.c_float, C.c_float, i32, u64, C.c_uint32,
                                           C.c_uint32, vp, vp, vp, vp, vp]
+    lib.metasd_verify_probs.argtypes = ([vp] + [i32] * 5 + [vp, i64, i64] * 2 + [vp] * 5 + [u64] + [vp] * 6)
+    lib.metasd_cache_workspace_bytes.argtypes = [i32, i32]
+    lib.metasd_cache_workspace_bytes.restype = C.c_size_t
+    lib.metasd_cache_plan.argtypes = [vp, i32, vp, vp, i64, vp, i32] + [vp] * 8
+    lib.metasd_cache_release.argtypes = [vp, i32, vp, i64, vp]
     lib.metasd_strerror.argtypes = [C.c_int]
     lib.metasd_strerror.restype = C.c_char_p
     lib.verify_noalloc_at = C.cast(lib.metasd_verify_noalloc, C.c_void_p).value
+    lib.verify_probs_at = C.cast(lib.metasd_verify_probs, C.c_void_p).value
+    lib.cache_plan_at = C.cast(lib.metasd_cache_plan, C.c_void_p).value
+    lib.cache_release_at = C.cast(lib.metasd_cache_release, C.c_void_p).value
     if path == LIB_PATH:
         try:
             from . import _call
@@ -155,6 +175,95 @@ class VerifyResult:
         """p_x, q_x, D, u as fp32 [B,k] and accept as int32 [B,k]."""
         d = self.diag
         return d[..., 0], d[..., 1], d[..., 2], d[..., 3], d[..., 4].contiguous().view(torch.int32)
+
+
+@dataclass
+class ProbsResult:
+    accepted_len: torch.Tensor   # [B] int32
+    next_token: torch.Tensor     # [B] int32
+    d_tv: Optional[torch.Tensor] = None     # [B, k] fp32
+    reward: Optional[torch.Tensor] = None   # [B] fp32, of a context's round
+
+
+def _expect(name: str, t, dtype, shape, device: torch.device):
+    """The library sees addresses only: what they lead to is checked here."""
+    if t.dtype != dtype or tuple(t.shape) != shape or t.device != device or not t.is_contiguous():
+        raise ValueError("%s: a contiguous %s tensor of shape %s on %s is due, not %s of shape %s on %s" % (
+            name, dtype, shape, device, t.dtype, tuple(t.shape), t.device))
+
+
+def _strides(name: str, t, dtype, B: int, rows: int, V: int, device: torch.device):
+    """Strides of sequences and rows, in entries; rows may be apart, their entries may not."""
+    if t.dtype != dtype or t.shape != (B, rows, V) or t.device != device:
+        raise ValueError("%s: a %s tensor of shape %s on %s is due, not %s of shape %s on %s" % (
+            name, dtype, (B, rows, V), device, t.dtype, tuple(t.shape), t.device))
+    seq, row, entry = t.stride()
+    if entry != 1 and V > 1:
+        raise ValueError("%s: a row's entries have to lie next to each other (stride %d)" % (name, entry))
+    return seq, row
+
+
+def _verify_probs(ctx, target, draft, tokens, u_accept, u_draw, draft_len, draft_place, seed, out, want_d_tv, status):
+    if not target.is_cuda or target.dim() != 3 or target.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("target_probs: a CUDA tensor [B, k + 1, V] of bf16 or fp32 is due")
+    dev = target.device
+    B, rows, V = target.shape
+    k, i32, f32 = rows - 1, torch.int32, torch.float32
+    tss, trs = _strides("target_probs", target, target.dtype, B, rows, V, dev)
+    dss = drs = 0
+    if draft is not None:
+        dss, drs = _strides("draft_probs", draft, target.dtype, B, k, V, dev)
+    if k > 0:
+        _expect("draft_tokens", tokens, i32, (B, k), dev)
+        _expect("u_accept", u_accept, f32, (B, k), dev)
+    else:
+        tokens = u_accept = draft = None
+    _expect("u_draw", u_draw, f32, (B,), dev)
+    if draft_len is not None:
+        _expect("draft_len", draft_len, i32, (B,), dev)
+    if draft_place is not None:
+        _expect("draft_place", draft_place, i32, (B,), dev)
+    if status is not None and (status.dtype != i32 or status.device != dev or status.numel() < 1):
+        raise ValueError("status: an int32 tensor on %s is due" % dev)
+    if out is None:
+        out = ProbsResult(torch.empty(B, dtype=i32, device=dev), torch.empty(B, dtype=i32, device=dev))
+    else:
+        _expect("accepted_len", out.accepted_len, i32, (B,), dev)
+        _expect("next_token", out.next_token, i32, (B,), dev)
+    if want_d_tv and out.d_tv is None:
+        out.d_tv = torch.zeros((B, k), dtype=f32, device=dev)
+    elif want_d_tv:
+        _expect("d_tv", out.d_tv, f32, (B, k), dev)
+    d_tv = out.d_tv if want_d_tv and k > 0 else None
+    reward = None
+    if ctx is not None:
+        if out.reward is None:
+            out.reward = torch.empty(B, dtype=f32, device=dev)
+        else:
+            _expect("reward", out.reward, f32, (B,), dev)
+        reward = out.reward
+    lib = _lib or load_library()
+    args = (ctx, dev.index, B, k, V, DTYPES[target.dtype], target, tss, trs, draft, dss, drs, draft_place, tokens, draft_len, u_accept,
+            u_draw, seed, out.accepted_len, out.next_token, d_tv, reward, status, _stream(dev))
+    rc = NotImplemented
+    if _call is not None:
+        rc = _call.verify_probs(lib.verify_probs_at, *args)
+    if rc is NotImplemented:
+        rc = lib.metasd_verify_probs(*[_ptr(a) if isinstance(a, torch.Tensor) else a for a in args])
+    if rc != OK:
+        raise MetasdError(rc, "metasd_verify_probs")
+    return out
+
+
+def verify_probs(target_probs: torch.Tensor, draft_probs: Optional[torch.Tensor], draft_tokens: Optional[torch.Tensor],
+                 u_accept: Optional[torch.Tensor], u_draw: torch.Tensor, draft_len: Optional[torch.Tensor] = None,
+                 draft_place: Optional[torch.Tensor] = None, want_d_tv: bool = False, out: Optional[ProbsResult] = None,
+                 status: Optional[torch.Tensor] = None) -> ProbsResult:
+    """metasd_verify_probs without a context, on the device of target_probs and its current stream: target_probs [B, k+1, V],
+    draft_probs [B, k, V] (None: drafters that were certain of their tokens), bf16 or fp32, rows of any strides; draft_tokens
+    [B, k] int32; u_accept [B, k] and u_draw [B] fp32 uniforms.  k = 0 draws a token from every target row."""
+    return _verify_probs(None, target_probs, draft_probs, draft_tokens, u_accept, u_draw, draft_len, draft_place, 0, out,
+                         want_d_tv, status)
 
 
 class MetaSD:
@@ -247,6 +356,17 @@ class MetaSD:
             raise MetasdError(rc, "metasd_verify")
         return out
 
+    def verify_probs(self, target_probs: torch.Tensor, draft_probs: Optional[torch.Tensor], draft_tokens: torch.Tensor,
+                     u_accept: torch.Tensor, u_draw: torch.Tensor, seed: int = 0, draft_len: Optional[torch.Tensor] = None,
+                     draft_place: Optional[torch.Tensor] = None, want_d_tv: bool = False,
+                     out: Optional[ProbsResult] = None) -> ProbsResult:
+        """A round of this context from probabilities and given random numbers (the function of the same name): its reward feeds
+        the bandits, seed keys the randomised policies' arms."""
+        if self._at is None:
+            raise MetasdError(ERR_INVALID_ARGUMENT, "metasd_verify_probs on a closed context")
+        return _verify_probs(self._at, target_probs, draft_probs, draft_tokens, u_accept, u_draw, draft_len, draft_place, seed,
+                             out, want_d_tv, None)
+
     def verify_host(self, target_logits: torch.Tensor, draft_logits: torch.Tensor,
                     draft_tokens: torch.Tensor, temperature: float, seed: int,
                     accepted_len: torch.Tensor, next_token: torch.Tensor, reward: torch.Tensor,
@@ -316,6 +436,120 @@ def verify_noalloc(target_logits: torch.Tensor, draft_logits: torch.Tensor, draf
         temperature, reward_temperature, reward_kind, seed,
         sequence_base, round_, _ptr(accepted_len), _ptr(next_token), _ptr(reward),
         _ptr(status), _stream(dev))
+
+
+@dataclass
+class CachePlan:
+    """Outputs of BlockCache.plan; those that are None are not asked for (token_start and slot_map are due)."""
+    order: Optional[torch.Tensor]         # [B] int32: sequences by pool
+    place: Optional[torch.Tensor]         # [B] int32: its inverse
+    pool_start: Optional[torch.Tensor]    # [n_pools + 1] int32
+    token_start: torch.Tensor             # [B + 1] int32, by place
+    slot_map: torch.Tensor                # [max_tokens] int64
+    position: Optional[torch.Tensor]      # [max_tokens] int32
+    sequence: Optional[torch.Tensor]      # [max_tokens] int32
+
+
+class BlockCache:
+    """The block tables and free lists of the paged caches of n_pools models (``metasd_cache``), in the caller's tensors."""
+
+    def __init__(self, block_table: torch.Tensor, held: torch.Tensor, free_blocks: torch.Tensor, free_count: torch.Tensor,
+                 page_size: int, status: Optional[torch.Tensor] = None):
+        """block_table [n_pools, max_batch, max_blocks], held [n_pools, max_batch], free_blocks [n_pools, n_blocks] and
+        free_count [n_pools], all int32 on one device; see BlockCache.empty for caches that hold nothing."""
+        if block_table.dim() != 3 or free_blocks.dim() != 2 or not block_table.is_cuda:
+            raise ValueError("block_table [n_pools, max_batch, max_blocks] and free_blocks [n_pools, n_blocks] are due, on a CUDA device")
+        P, B, M = block_table.shape
+        dev, i32 = block_table.device, torch.int32
+        _expect("block_table", block_table, i32, (P, B, M), dev)
+        _expect("held", held, i32, (P, B), dev)
+        _expect("free_blocks", free_blocks, i32, (P, free_blocks.shape[1]), dev)
+        _expect("free_count", free_count, i32, (P,), dev)
+        if status is None:
+            status = torch.zeros(1, dtype=i32, device=dev)
+        _expect("status", status, i32, (1,), dev)
+        self.lib = load_library()
+        n = self.lib.metasd_cache_workspace_bytes(B, P)
+        if n == 0 or page_size < 1:
+            raise MetasdError(ERR_INVALID_ARGUMENT, "metasd_cache_workspace_bytes")
+        self.block_table, self.held, self.free_blocks, self.free_count, self.status = block_table, held, free_blocks, free_count, status
+        self.workspace = torch.empty(n, dtype=torch.uint8, device=dev)
+        self.device, self.n_pools, self.max_batch, self.page_size = dev, P, B, int(page_size)
+        self._c = MetasdCache(*[t.data_ptr() for t in (block_table, held, free_blocks, free_count, self.workspace, status)],
+                              P, B, M, free_blocks.shape[1], self.page_size, dev.index)
+        self._at = C.addressof(self._c)
+
+    @classmethod
+    def empty(cls, n_pools: int, max_batch: int, max_blocks: int, n_blocks: int, page_size: int, device: int = 0) -> "BlockCache":
+        """Caches without entries; every pool has the blocks 0 .. n_blocks - 1."""
+        dev, i32 = torch.device("cuda", device), torch.int32
+        free = torch.arange(n_blocks - 1, -1, -1, dtype=i32, device=dev).repeat(n_pools, 1)
+        return cls(torch.full((n_pools, max_batch, max_blocks), -1, dtype=i32, device=dev),
+                   torch.zeros((n_pools, max_batch), dtype=i32, device=dev), free,
+                   torch.full((n_pools,), n_blocks, dtype=i32, device=dev), page_size)
+
+    def _per_pool(self, name: str, t: torch.Tensor, B: int) -> int:
+        """Entries between pools: of a [B] tensor (the same for all) or an [n_pools, B] one."""
+        _expect(name, t, torch.int32, (B,) if t.dim() == 1 else (self.n_pools, B), self.device)
+        return 0 if t.dim() == 1 else B
+
+    def plan(self, length: torch.Tensor, cached: torch.Tensor, pool: Optional[torch.Tensor] = None,
+             max_tokens: Optional[int] = None, out: Optional[CachePlan] = None) -> CachePlan:
+        """metasd_cache_plan: length [B], cached [B] or [n_pools, B], pool [B] (None: pool 0), int32.  max_tokens: entries that the
+        outputs have room for, where they are not given."""
+        dev, i32 = self.device, torch.int32
+        B = length.shape[0]
+        _expect("length", length, i32, (B,), dev)
+        stride = self._per_pool("cached", cached, B)
+        if pool is not None:
+            _expect("pool", pool, i32, (B,), dev)
+        if out is None:
+            if max_tokens is None:
+                raise ValueError("max_tokens or the outputs are due")
+            def ints(*shape):
+                return torch.empty(shape, dtype=i32, device=dev)
+            out = CachePlan(ints(B), ints(B), ints(self.n_pools + 1), ints(B + 1),
+                            torch.empty(max_tokens, dtype=torch.int64, device=dev), ints(max_tokens), ints(max_tokens))
+        else:
+            room = out.slot_map.shape[0]
+            if max_tokens is not None and max_tokens != room:
+                raise ValueError("slot_map has room for %d entries, not %d" % (room, max_tokens))
+            max_tokens = room
+            _expect("slot_map", out.slot_map, torch.int64, (room,), dev)
+            _expect("token_start", out.token_start, i32, (B + 1,), dev)
+            for name, t, shape in (("order", out.order, (B,)), ("place", out.place, (B,)), ("pool_start", out.pool_start, (self.n_pools + 1,)),
+                                   ("position", out.position, (room,)), ("sequence", out.sequence, (room,))):
+                if t is not None:
+                    _expect(name, t, i32, shape, dev)
+        args = (self._at, B, pool, cached, stride, length, max_tokens, out.order, out.place, out.pool_start, out.token_start, out.slot_map,
+                out.position, out.sequence, _stream(dev))
+        rc = NotImplemented
+        if _call is not None:
+            rc = _call.cache_plan(self.lib.cache_plan_at, *args)
+        if rc is NotImplemented:
+            rc = self.lib.metasd_cache_plan(*[_ptr(a) if isinstance(a, torch.Tensor) else a for a in args])
+        if rc != OK:
+            raise MetasdError(rc, "metasd_cache_plan")
+        return out
+
+    def release(self, keep: torch.Tensor):
+        """metasd_cache_release: keep [B] (all pools) or [n_pools, B] int32, the entries that stay."""
+        B = keep.shape[-1]
+        stride = self._per_pool("keep", keep, B)
+        args = (self._at, B, keep, stride, _stream(self.device))
+        rc = NotImplemented
+        if _call is not None:
+            rc = _call.cache_release(self.lib.cache_release_at, *args)
+        if rc is NotImplemented:
+            rc = self.lib.metasd_cache_release(*[_ptr(a) if isinstance(a, torch.Tensor) else a for a in args])
+        if rc != OK:
+            raise MetasdError(rc, "metasd_cache_release")
+
+    def last_status(self) -> int:
+        """Reads and clears the status word (synchronises)."""
+        flags = int(self.status.item())
+        self.status.zero_()
+        return flags
 
 
 def state_validate(cfg: MetasdConfig, blob: bytes) -> int:

@@ -369,6 +369,117 @@ int metasd_verify_host(metasd_ctx *ctx, int32_t batch, int32_t k, const void *ho
     return METASD_OK;
 }
 
+int metasd_verify_probs(metasd_ctx *ctx, int32_t device, int32_t batch, int32_t k, int32_t vocab, int32_t prob_dtype,
+                        const void *target_probs, int64_t target_seq_stride, int64_t target_row_stride, const void *draft_probs,
+                        int64_t draft_seq_stride, int64_t draft_row_stride, const int32_t *draft_place,
+                        const int32_t *draft_tokens, const int32_t *draft_len, const float *u_accept, const float *u_draw,
+                        uint64_t seed, int32_t *accepted_len, int32_t *next_token, float *d_tv, float *reward, uint32_t *status,
+                        void *stream)
+{
+    if (batch < 1 || batch > 65535 || k < 0 || k > 16 || vocab < 1) return METASD_ERR_INVALID_ARGUMENT;
+    if (vocab > (1 << 30)) return METASD_ERR_UNSUPPORTED;
+    if (prob_dtype != METASD_BF16 && prob_dtype != METASD_FP32) return METASD_ERR_UNSUPPORTED;
+    if (!target_probs || !u_draw || !accepted_len || !next_token) return METASD_ERR_INVALID_ARGUMENT;
+    if (k > 0 && (!draft_tokens || !u_accept)) return METASD_ERR_INVALID_ARGUMENT;
+    if (target_seq_stride < 0 || target_row_stride < 0 || draft_seq_stride < 0 || draft_row_stride < 0) return METASD_ERR_INVALID_ARGUMENT;
+    const uintptr_t in_entry = logit_size(prob_dtype) - 1;
+    if (((uintptr_t)target_probs & in_entry) != 0 || ((uintptr_t)draft_probs & in_entry) != 0) return METASD_ERR_INVALID_ARGUMENT;
+    if (ctx) {
+        const metasd_config &cfg = ctx->cfg;
+        if (device != cfg.device || batch > cfg.max_batch || k < 1 || k > cfg.max_draft || vocab != cfg.vocab || !reward || status)
+            return METASD_ERR_INVALID_ARGUMENT;
+    } else if (reward) {
+        return METASD_ERR_INVALID_ARGUMENT;
+    }
+    DeviceScope scope(device);
+    if (scope.error != cudaSuccess) { (void)cudaGetLastError(); return METASD_ERR_CUDA; }
+    int n_sm = 0;
+    CK(cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, device));
+
+    ProbsParams p;
+    memset(&p, 0, sizeof p);
+    p.batch = batch; p.k = k; p.V = vocab;
+    p.min_draft = ctx ? 1 : 0;
+    p.target = target_probs; p.target_seq = target_seq_stride; p.target_row = target_row_stride;
+    p.draft = draft_probs; p.draft_seq = draft_seq_stride; p.draft_row = draft_row_stride;
+    p.place = draft_place; p.tokens = draft_tokens; p.draft_len = draft_len || !ctx ? draft_len : ctx->draft_len;
+    p.u_accept = u_accept; p.u_draw = u_draw;
+    p.accepted_len = accepted_len; p.next_token = next_token;
+    // the block-divergence reward is made from the distances: where the caller wants none they go to the context's scratch
+    const bool feeds_bd = ctx && ctx->cfg.reward == METASD_REWARD_BD;
+    p.d_tv = k == 0 ? nullptr : d_tv || !feeds_bd ? d_tv : reinterpret_cast<float *>(ctx->stats);
+    p.status = ctx ? ctx->status : status;
+    CK(launch_probs(p, prob_dtype, n_sm, (cudaStream_t)stream));
+    if (!ctx) return METASD_OK;
+    ctx->launches += 1;
+
+    VerifyParams v;
+    memset(&v, 0, sizeof v);
+    v.batch = batch; v.k = k; v.V = vocab;
+    v.K = ctx->cfg.n_drafters; v.bandit = ctx->cfg.bandit; v.reward_kind = ctx->cfg.reward; v.tau = ctx->cfg.window;
+    v.sequence_base = ctx->cfg.sequence_base; v.seed = seed; v.beta = ctx->cfg.beta; v.gamma = ctx->cfg.gamma;
+    v.draft_len = p.draft_len; v.accepted_len = accepted_len; v.reward = reward; v.st = ctx->st;
+    CK(launch_feedback(v, p.d_tv, (cudaStream_t)stream));
+    ctx->launches += 1;
+    return METASD_OK;
+}
+
+static int check_cache(const metasd_cache *c, int32_t batch)
+{
+    if (!c || !c->block_table || !c->held || !c->free_blocks || !c->free_count || !c->workspace) return METASD_ERR_INVALID_ARGUMENT;
+    if (c->n_pools < 1 || c->n_pools > METASD_MAX_POOLS || c->max_batch < 1 || c->max_batch > 65535) return METASD_ERR_INVALID_ARGUMENT;
+    if (c->max_blocks < 1 || c->n_blocks < 1 || c->page_size < 1) return METASD_ERR_INVALID_ARGUMENT;
+    if (((uintptr_t)c->workspace & 15) != 0 || batch < 1 || batch > c->max_batch) return METASD_ERR_INVALID_ARGUMENT;
+    return METASD_OK;
+}
+
+size_t metasd_cache_workspace_bytes(int32_t max_batch, int32_t n_pools)
+{
+    if (max_batch < 1 || max_batch > 65535 || n_pools < 1 || n_pools > METASD_MAX_POOLS) return 0;
+    return cache_workspace_bytes(max_batch, n_pools);
+}
+
+int metasd_cache_plan(const metasd_cache *cache, int32_t batch, const int32_t *pool, const int32_t *cached, int64_t cached_pool_stride,
+                      const int32_t *length, int32_t max_tokens, int32_t *order, int32_t *place, int32_t *pool_start,
+                      int32_t *token_start, int64_t *slot_map, int32_t *position, int32_t *sequence, void *stream)
+{
+    const int rc = check_cache(cache, batch);
+    if (rc != METASD_OK) return rc;
+    if (!cached || !length || !token_start || !slot_map || max_tokens < 1 || cached_pool_stride < 0) return METASD_ERR_INVALID_ARGUMENT;
+    DeviceScope scope(cache->device);
+    if (scope.error != cudaSuccess) { (void)cudaGetLastError(); return METASD_ERR_CUDA; }
+    int n_sm = 0;
+    CK(cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, cache->device));
+    CachePlanParams p;
+    memset(&p, 0, sizeof p);
+    p.c = *cache;
+    p.batch = batch; p.max_tokens = max_tokens;
+    p.page_inverse = inverse_of((uint32_t)cache->page_size);
+    p.wide = ((uintptr_t)slot_map & 15) == 0 && (((uintptr_t)position | (uintptr_t)sequence) & 7) == 0;
+    p.pool = pool; p.cached = cached; p.length = length; p.cached_pool = cached_pool_stride;
+    p.order = order; p.place = place; p.pool_start = pool_start; p.token_start = token_start;
+    p.slot_map = slot_map; p.position = position; p.sequence = sequence;
+    CK(launch_cache_plan(p, n_sm, (cudaStream_t)stream));
+    return METASD_OK;
+}
+
+int metasd_cache_release(const metasd_cache *cache, int32_t batch, const int32_t *keep, int64_t keep_pool_stride, void *stream)
+{
+    const int rc = check_cache(cache, batch);
+    if (rc != METASD_OK) return rc;
+    if (!keep || keep_pool_stride < 0) return METASD_ERR_INVALID_ARGUMENT;
+    DeviceScope scope(cache->device);
+    if (scope.error != cudaSuccess) { (void)cudaGetLastError(); return METASD_ERR_CUDA; }
+    CacheReleaseParams p;
+    memset(&p, 0, sizeof p);
+    p.c = *cache;
+    p.batch = batch;
+    p.page_inverse = inverse_of((uint32_t)cache->page_size);
+    p.keep = keep; p.keep_pool = keep_pool_stride;
+    CK(launch_cache_release(p, (cudaStream_t)stream));
+    return METASD_OK;
+}
+
 size_t metasd_state_bytes(const metasd_ctx *ctx) { return ctx ? blob_bytes(ctx->cfg) : 0; }
 
 int metasd_state_export(metasd_ctx *ctx, void *host_buf, size_t bytes, void *stream)

@@ -55,7 +55,7 @@ static int as_float(PyObject *o, float *out)
     return 1;
 }
 
-#define MOST 20
+#define MOST 25
 
 /* Converts the arguments by their kinds: a address (of a function, a context or a stream), t tensor, i whole number, f float.
  * Returns as as_address does. */
@@ -114,10 +114,45 @@ static PyObject *call_verify_noalloc(PyObject *self, PyObject *const *args, Py_s
     return PyLong_FromLong(rc);
 }
 
+static PyObject *call_verify_probs(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    CONVERTED("aaiiiiitiitiitttttittttta");
+    __typeof__(&metasd_verify_probs) verify = p[0];
+    Py_BEGIN_ALLOW_THREADS
+    rc = verify(p[1], (int32_t)i[2], (int32_t)i[3], (int32_t)i[4], (int32_t)i[5], (int32_t)i[6], p[7], (int64_t)i[8], (int64_t)i[9],
+                p[10], (int64_t)i[11], (int64_t)i[12], p[13], p[14], p[15], p[16], p[17], i[18], p[19], p[20], p[21], p[22], p[23],
+                p[24]);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+static PyObject *call_cache_plan(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    CONVERTED("aaittitittttttta");
+    __typeof__(&metasd_cache_plan) plan = p[0];
+    Py_BEGIN_ALLOW_THREADS
+    rc = plan(p[1], (int32_t)i[2], p[3], p[4], (int64_t)i[5], p[6], (int32_t)i[7], p[8], p[9], p[10], p[11], p[12], p[13], p[14], p[15]);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+static PyObject *call_cache_release(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    CONVERTED("aaitia");
+    __typeof__(&metasd_cache_release) release = p[0];
+    Py_BEGIN_ALLOW_THREADS
+    rc = release(p[1], (int32_t)i[2], p[3], (int64_t)i[4], p[5]);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
 static PyMethodDef methods[] = {
     {"verify", (PyCFunction)(void (*)(void))call_verify, METH_FASTCALL, "metasd_verify; its address comes first"},
     {"select", (PyCFunction)(void (*)(void))call_select, METH_FASTCALL, "metasd_select; its address comes first"},
     {"verify_noalloc", (PyCFunction)(void (*)(void))call_verify_noalloc, METH_FASTCALL, "metasd_verify_noalloc; its address comes first"},
+    {"verify_probs", (PyCFunction)(void (*)(void))call_verify_probs, METH_FASTCALL, "metasd_verify_probs; its address comes first"},
+    {"cache_plan", (PyCFunction)(void (*)(void))call_cache_plan, METH_FASTCALL, "metasd_cache_plan; its address comes first"},
+    {"cache_release", (PyCFunction)(void (*)(void))call_cache_release, METH_FASTCALL, "metasd_cache_release; its address comes first"},
     {NULL, NULL, 0, NULL},
 };
 

@@ -116,6 +116,43 @@ bool fused_supported(int dtype, int V, int k);
 cudaError_t fused_prepare(int device, int dtype, int V, int max_batch, int pin_cluster, int pin_threads, FusedPlan *plan);
 cudaError_t launch_fused(const VerifyParams &p, int dtype, const FusedPlan &plan, cudaStream_t stream,
                          uint64_t *launches);
+// verification from probabilities (metasd_probs.cu); strides in entries
+struct ProbsParams {
+    int32_t batch, k, V;
+    int32_t min_draft;        // what a sequence's draft length is clamped to from below
+    const void *target, *draft;
+    int64_t target_seq, target_row, draft_seq, draft_row;
+    const int32_t *place, *tokens, *draft_len;
+    const float *u_accept, *u_draw;
+    int32_t *accepted_len, *next_token;
+    float *d_tv;
+    uint32_t *status;
+    int32_t parts, part_vecs; // of a row: how many, and the 16-byte vectors of each; set by the launcher
+};
+cudaError_t launch_probs(const ProbsParams &p, int dtype, int n_sm, cudaStream_t stream);
+cudaError_t launch_feedback(const VerifyParams &p, const float *d_tv, cudaStream_t stream);   // reward, bandit update, next selection
+// paged caches (metasd_cache.cu)
+struct CachePlanParams {
+    metasd_cache c;
+    int32_t batch, max_tokens;
+    uint32_t page_inverse;    // inverse_of(page_size)
+    int32_t wide;             // entries may be written in pairs
+    const int32_t *pool, *cached, *length;
+    int64_t cached_pool;
+    int32_t *order, *place, *pool_start, *token_start;
+    int64_t *slot_map;
+    int32_t *position, *sequence;
+};
+struct CacheReleaseParams {
+    metasd_cache c;
+    int32_t batch;
+    uint32_t page_inverse;
+    const int32_t *keep;
+    int64_t keep_pool;
+};
+size_t cache_workspace_bytes(int max_batch, int n_pools);
+cudaError_t launch_cache_plan(const CachePlanParams &p, int n_sm, cudaStream_t stream);
+cudaError_t launch_cache_release(const CacheReleaseParams &p, cudaStream_t stream);
 // small state kernels (metasd_streaming.cu)
 cudaError_t launch_select(const BanditState &st, int batch, int32_t *arm_out, cudaStream_t stream);
 cudaError_t launch_reset(const BanditState &st, int max_batch, int K, int tau, int variant, double gamma,

@@ -1,0 +1,130 @@
+"""Refusals of metasd_verify_probs, metasd_cache_plan and metasd_cache_release, on the host: before any CUDA call, so that they are
+the same with and without a device; and the plain walks that the GPU tests compare with, on cases worked by hand."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+import _probs_reference as R
+from _cache_reference import Caches
+from paper_2604_05417_b200 import binding as M
+from paper_2604_05417_b200 import build as B
+
+
+@pytest.fixture(scope="module")
+def lib():
+    B.build()
+    return M.load_library()
+
+
+BUFFER = C.create_string_buffer(256)
+AT = (C.addressof(BUFFER) + 15) // 16 * 16      # an aligned address; no call below gets as far as using it
+
+
+def probs_call(lib, **kw):
+    a = dict(ctx=None, device=0, batch=4, k=2, vocab=10, dtype=M.FP32, target=AT, tss=30, trs=10, draft=AT, dss=20, drs=10, place=None,
+             tokens=AT, draft_len=None, ua=AT, ud=AT, seed=0, acc=AT, tok=AT, d_tv=None, reward=None, status=None, stream=None)
+    assert set(kw) <= set(a)
+    return lib.metasd_verify_probs(*dict(a, **kw).values())
+
+
+def test_verify_probs_checks_its_arguments(lib):
+    for kw in (dict(batch=0), dict(batch=65536), dict(k=-1), dict(k=17), dict(vocab=0), dict(target=None), dict(ud=None), dict(acc=None),
+               dict(tok=None), dict(tokens=None), dict(ua=None), dict(tss=-1), dict(trs=-1), dict(dss=-1), dict(drs=-1),
+               dict(target=AT + 2), dict(draft=AT + 1), dict(dtype=M.BF16, target=AT + 1), dict(reward=AT)):
+        assert probs_call(lib, **kw) == M.ERR_INVALID_ARGUMENT, kw
+    for kw in (dict(dtype=2), dict(dtype=-1), dict(vocab=(1 << 30) + 1)):
+        assert probs_call(lib, **kw) == M.ERR_UNSUPPORTED, kw
+
+
+def cache_struct(**kw):
+    a = dict(block_table=AT, held=AT, free_blocks=AT, free_count=AT, workspace=AT, status=None, n_pools=2, max_batch=8, max_blocks=4,
+             n_blocks=30, page_size=8, device=0)
+    assert set(kw) <= set(a)
+    return M.MetasdCache(**dict(a, **kw))
+
+
+BAD_CACHES = [dict(block_table=None), dict(held=None), dict(free_blocks=None), dict(free_count=None), dict(workspace=None),
+              dict(workspace=AT + 8), dict(n_pools=0), dict(n_pools=33), dict(max_batch=0), dict(max_batch=65536), dict(max_blocks=0),
+              dict(n_blocks=0), dict(page_size=0), dict(page_size=-1)]
+
+
+def test_cache_calls_check_their_arguments(lib):
+    def plan(cache, **kw):
+        a = dict(batch=4, pool=None, cached=AT, stride=0, length=AT, max_tokens=16, order=None, place=None, pool_start=None,
+                 token_start=AT, slot_map=AT, position=None, sequence=None, stream=None)
+        assert set(kw) <= set(a)
+        return lib.metasd_cache_plan(None if cache is None else C.byref(cache), *dict(a, **kw).values())
+
+    def release(cache, batch=4, keep=AT, stride=0):
+        return lib.metasd_cache_release(None if cache is None else C.byref(cache), batch, keep, stride, None)
+
+    for kw in BAD_CACHES:
+        assert plan(cache_struct(**kw)) == M.ERR_INVALID_ARGUMENT, kw
+        assert release(cache_struct(**kw)) == M.ERR_INVALID_ARGUMENT, kw
+    assert plan(None) == release(None) == M.ERR_INVALID_ARGUMENT
+    good = cache_struct()
+    for kw in (dict(batch=0), dict(batch=9), dict(cached=None), dict(length=None), dict(token_start=None), dict(slot_map=None),
+               dict(max_tokens=0), dict(stride=-1)):
+        assert plan(good, **kw) == M.ERR_INVALID_ARGUMENT, kw
+    for kw in (dict(batch=0), dict(batch=9), dict(keep=None), dict(stride=-1)):
+        assert release(good, **kw) == M.ERR_INVALID_ARGUMENT, kw
+    for n, p in ((0, 1), (65536, 1), (1, 0), (1, 33), (-1, -1)):
+        assert lib.metasd_cache_workspace_bytes(n, p) == 0
+    assert lib.metasd_cache_workspace_bytes(100, 3) >= 100 * 3 * 16 and lib.metasd_cache_workspace_bytes(1, 1) > 0
+
+
+def test_the_cache_mirror_matches_the_header():
+    assert C.sizeof(M.MetasdCache) == 6 * 8 + 6 * 4
+
+
+def test_tensors_on_the_host_are_refused(lib):
+    t = torch.zeros((2, 2, 8))
+    with pytest.raises(ValueError):
+        M.verify_probs(t, t[:, :1], torch.zeros((2, 1), dtype=torch.int32), torch.zeros((2, 1)), torch.zeros(2))
+    i = torch.zeros((1, 2, 3), dtype=torch.int32)
+    with pytest.raises(ValueError):
+        M.BlockCache(i, i[:, :, 0], i[:, 0], i[:, 0, 0], 8)
+
+
+def test_calls_convert_as_ctypes_does(lib):
+    """The extension module's calls: the library's own answers, and NotImplemented for what it leaves to ctypes."""
+    if M._call is None:
+        pytest.skip("not built for this interpreter")
+    t = torch.zeros(8, dtype=torch.int32)
+    probs = [lib.verify_probs_at, None, 0, 0, 1, 8, M.FP32, t, 8, 8, t, 8, 8, None, t, None, t, t, 0, t, t, None, None, None, None]
+    plan = [lib.cache_plan_at, None, 1, None, t, 0, t, 8, None, None, None, t, t, None, None, None]
+    release = [lib.cache_release_at, None, 1, t, 0, None]
+    for fn, args, tensors in ((M._call.verify_probs, probs, (7, 10, 14, 16, 17, 19, 20)), (M._call.cache_plan, plan, (4, 6, 11, 12)),
+                              (M._call.cache_release, release, (3,))):
+        assert fn(*args) == M.ERR_INVALID_ARGUMENT      # no sequences; no cache
+        for at in tensors:
+            with pytest.raises(AttributeError):
+                fn(*(args[:at] + [12345] + args[at + 1:]))
+        assert fn(*(args[:2] + [1.0] + args[3:])) is NotImplemented
+        with pytest.raises(TypeError):
+            fn(*args[:-1])
+
+
+def test_reference_verification_by_hand():
+    p = np.array([[[0.5, 0.25, 0.25], [0.0, 1.0, 0.0]]])
+    q = np.array([[[0.25, 0.75, 0.0]]])
+    x = np.array([[1]])
+    for u, accepted in ((0.33, 1), (1 / 3 + 1e-9, 0)):      # p/q = 1/3
+        a, token, d, _ = R.verify(p, q, x, np.array([[u]]), np.array([0.4]))
+        # rejected: (0.25, 0, 0.25) is left, 0.4 of it lies in its first half
+        assert a[0] == accepted and token[0] == (1 if accepted else 0) and d[0, 0] == 0.5
+    assert R.verify(p, q, x, np.array([[0.9]]), np.array([0.5]))[1][0] == 2       # strictly above half
+    a, token, d, _ = R.verify(p, None, x, np.array([[0.9]]), np.array([0.9]))      # certain of token 1
+    assert a[0] == 0 and token[0] == 2 and d[0, 0] == 0.75
+
+
+def test_reference_caches_by_hand():
+    c = Caches(2, 3, 4, 4, [[10, 11, 12], [20, 21]])
+    order, place, start, tokens, entries = c.plan([5, 1, 2], [[0] * 3] * 2, [1, 0, 1])
+    assert (order, place, start, tokens) == ([1, 0, 2], [1, 0, 2], [0, 1, 3], [0, 1, 6, 8])
+    # pool 0 gives block 12; pool 1 gives 21 and 20 to sequence 0 and has none left for sequence 2
+    assert [e[0] for e in entries] == [48, 84, 85, 86, 87, 80, -1, -1]
+    c.release([[0, 1, 0], [4, 0, 0]])
+    assert c.free == [[10, 11], [20]] and c.table[1][0] == [21]
