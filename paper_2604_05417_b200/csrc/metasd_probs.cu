@@ -6,8 +6,9 @@
 //   d_TV(p_j, q_j)        1/2 sum_v |p_j(v) - q_j(v)|                        (only where it is asked for)
 //
 // Whole numbers come out of sums over a row, so the sums are made as if in real numbers: with d = fl(p - q) the rounding error
-// (p - d) - q of a difference that is above zero is a float, exactly (p >= q >= 0); the d's are added up in fp64, the errors,
-// 2^-24 of them, in fp32: what is lost is below 2^-45 of the sum, and next to no draw is that near to an edge.
+// (p - d) - q of a difference that is above zero is a float, exactly (p >= q >= 0), and so is the rounding error of an addition
+// (Knuth's two-sum, six operations on a packed pair).  The errors, 2^-24 of what they belong to, are added up apart; what is lost
+// is theirs, below 2^-45 of the sum, and next to no draw is that near to an edge.  The lanes' sums join in fp64.
 //
 // Bound by memory: without distances one row pair per sequence is read (the one that the token is drawn from), with them every
 // pair.  A row is cut into parts by its length alone, a warp sums a part, and the parts' sums are put together in one order:
@@ -86,62 +87,127 @@ template <typename LT> __device__ __forceinline__ bool suspicious(const uint4 &v
 }
 __device__ __forceinline__ bool is_probability(float x) { return x >= 0.f && x < INFINITY; }   // -0 is one
 
-// Sums of a lane.
+// Sums of a lane, as packed pairs.
 struct Sums {
-    double weight;      // of max(0, p - q), the differences as rounded
-    float rest;         // what the roundings left out
-    float apart;        // of |p - q|
+    uint64_t over;      // of max(0, p - q), the differences as rounded, rounded again at every addition
+    uint64_t rest;      // what these roundings left out
+    uint64_t under;     // of max(0, q - p)
     bool bad;
 };
+
+__device__ __forceinline__ uint64_t sub2(uint64_t a, uint64_t b) { return fma2(b, pack2(-1.f), a); }
+__device__ __forceinline__ uint64_t max2(uint64_t a, uint64_t b)
+{
+    float al, ah, bl, bh;
+    unpack2(a, al, ah);
+    unpack2(b, bl, bh);
+    return pack2(fmaxf(al, bl), fmaxf(ah, bh));
+}
+// sum += x, and what the rounding takes away goes to rest (x and the sum in any order of size).
+__device__ __forceinline__ void add_exactly(uint64_t &sum, uint64_t &rest, uint64_t x)
+{
+    const uint64_t s = add2(sum, x), part = sub2(s, sum);
+    rest = add2(rest, add2(sub2(sum, sub2(s, part)), sub2(x, part)));
+    sum = s;
+}
+template <typename LT> __device__ __forceinline__ uint64_t pair_at(const uint4 &v, int i)   // entries 2 i, 2 i + 1
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    if constexpr (sizeof(LT) == 2) return pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
+    else return pack2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+}
+
+// A pair of entries of both rows.  With m = max(p, q), m - q is max(0, p - q) with no comparison of its own.
+template <bool TV> __device__ __forceinline__ void add_pair(Sums &s, uint64_t p, uint64_t q)
+{
+    const uint64_t m = max2(p, q), d = sub2(m, q);
+    s.rest = add2(s.rest, sub2(sub2(m, d), q));
+    add_exactly(s.over, s.rest, d);
+    if (TV) s.under = add2(s.under, sub2(m, p));
+}
 
 template <typename LT, bool PAIR, bool TV>
 __device__ __forceinline__ void add_vectors(Sums &s, const uint4 &ra, const uint4 &rd, int tok0, int certain)
 {
     constexpr int VEC = Logit<LT>::VEC;
-    float p[VEC], q[VEC];
-    Logit<LT>::unpack(ra, p);
-    if (PAIR) {
-        Logit<LT>::unpack(rd, q);
-    } else {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) q[e] = tok0 + e == certain ? 1.f : 0.f;
-    }
     if (suspicious<LT>(ra) || (PAIR && suspicious<LT>(rd))) {
+        float p[VEC], q[VEC];
+        Logit<LT>::unpack(ra, p);
+        Logit<LT>::unpack(rd, q);
 #pragma unroll
         for (int e = 0; e < VEC; ++e)
-            if (!is_probability(p[e]) || !is_probability(q[e])) s.bad = true;
+            if (!is_probability(p[e]) || (PAIR && !is_probability(q[e]))) s.bad = true;
     }
-    float apart = 0.f, rest = 0.f;
+    if (PAIR) {
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-        const float d = p[e] - q[e];
-        const bool left = d > 0.f;
-        s.weight += (double)(left ? d : 0.f);
-        rest += left ? (p[e] - d) - q[e] : 0.f;
-        if (TV) apart += fabsf(d);
+        for (int i = 0; i < VEC / 2; ++i) add_pair<TV>(s, pair_at<LT>(ra, i), pair_at<LT>(rd, i));
+    } else if (certain < tok0 || certain >= tok0 + VEC) {
+#pragma unroll
+        for (int i = 0; i < VEC / 2; ++i) add_exactly(s.over, s.rest, pair_at<LT>(ra, i));
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC / 2; ++i)
+            add_pair<TV>(s, pair_at<LT>(ra, i), pack2(certain == tok0 + 2 * i ? 1.f : 0.f, certain == tok0 + 2 * i + 1 ? 1.f : 0.f));
     }
-    s.rest += rest;
-    if (TV) s.apart += apart;
 }
 
+// The lane's sum of max(0, p - q) in fp64.
+__device__ __forceinline__ double weight_of(const Sums &s)
+{
+    float lo, hi;
+    unpack2(s.over, lo, hi);
+    const float sum = lo + hi, part = sum - lo;
+    return (double)sum + (double)(((lo - (sum - part)) + (hi - part)) + sum2(s.rest));
+}
+
+// The sums of the vectors g0 .. g1 - 1 (a multiple of 32 from g0), a lane every 32nd.  The order of additions does not depend on where the rows
+// start: off 16-byte boundaries a vector is two loads (the second one's line is in L1), so that half as many are in flight.
 template <typename LT, bool PAIR, bool TV, bool SHIFTED>
 __device__ __forceinline__ Sums sum_part(const PairOfRows<LT> &r, int g0, int g1)
 {
-    constexpr int VEC = Logit<LT>::VEC;
-    Sums s = {0.0, 0.f, 0.f, false};
-    for (int g = g0 + (threadIdx.x & 31); g < g1; g += 32 * BATCH) {
-        uint4 ra[BATCH], rd[BATCH];
+    constexpr int VEC = Logit<LT>::VEC, N = SHIFTED ? BATCH / 2 : BATCH;
+    Sums s = {0ull, 0ull, 0ull, false};
+    int g = g0 + (threadIdx.x & 31);
+    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+    // whole vectors, whole batches: nothing but loads and sums
+    for (int c = g0; c + 32 * N <= min(g1, r.V / VEC); c += 32 * N, g += 32 * N) {
+        uint4 ra[N], rd[N];
+        if (!SHIFTED) {
 #pragma unroll
-        for (int i = 0; i < BATCH; ++i) {
-            const int gi = g + 32 * i;
-            ra[i] = rd[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (gi < g1) {
-                ra[i] = vector_at<LT, SHIFTED, false>(r.a, r.lead_a, gi, r.V);
-                if (PAIR) rd[i] = vector_at<LT, SHIFTED, false>(r.d, r.lead_d, gi, r.V);
+            for (int i = 0; i < N; ++i) ra[i] = ld_stream(r.a + g + 32 * i);
+            if (PAIR) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) rd[i] = ld_stream(r.d + g + 32 * i);
+            }
+        } else {
+            uint4 na[N], nd[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                ra[i] = __ldg(r.a + g + 32 * i);
+                na[i] = r.lead_a ? __ldg(r.a + g + 32 * i + 1) : zero;
+            }
+            if (PAIR) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    rd[i] = __ldg(r.d + g + 32 * i);
+                    nd[i] = r.lead_d ? __ldg(r.d + g + 32 * i + 1) : zero;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                ra[i] = Logit<LT>::shifted(ra[i], na[i], r.lead_a);
+                if (PAIR) rd[i] = Logit<LT>::shifted(rd[i], nd[i], r.lead_d);
             }
         }
 #pragma unroll
-        for (int i = 0; i < BATCH; ++i) add_vectors<LT, PAIR, TV>(s, ra[i], rd[i], (g + 32 * i) * VEC, r.certain);
+        for (int i = 0; i < N; ++i) add_vectors<LT, PAIR, TV>(s, ra[i], PAIR ? rd[i] : zero, (g + 32 * i) * VEC, r.certain);
+    }
+    // the row's end
+#pragma unroll 1
+    for (; g < g1; g += 32) {
+        const uint4 ra = vector_at<LT, SHIFTED, false>(r.a, r.lead_a, g, r.V);
+        const uint4 rd = PAIR ? vector_at<LT, SHIFTED, false>(r.d, r.lead_d, g, r.V) : zero;
+        add_vectors<LT, PAIR, TV>(s, ra, rd, g * VEC, r.certain);
     }
     return s;
 }
@@ -153,69 +219,67 @@ __device__ __forceinline__ Sums sum_part(const PairOfRows<LT> &r, bool pair, int
     return r.lead_a == 0 ? sum_part<LT, false, TV, false>(r, g0, g1) : sum_part<LT, false, TV, true>(r, g0, g1);
 }
 
+// Inclusive sums over the lanes.
+__device__ __forceinline__ double lanes_up_to(double x)
+{
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const double t = __shfl_up_sync(FULL, x, o);
+        if (lane >= o) x += t;
+    }
+    return x;
+}
+// The lane in whose x, laid end to end (upto: their inclusive sums), the threshold lies: the first that ends beyond it; rounding
+// may leave none, then the last with weight; -1: no weight.
+__device__ __forceinline__ int crossing_lane(double x, double upto, double threshold, bool &beyond)
+{
+    const unsigned mass = __ballot_sync(FULL, x > 0.0), hits = __ballot_sync(FULL, upto > threshold) & mass;
+    beyond = hits != 0;
+    return hits ? __ffs(hits) - 1 : 31 - __clz(mass);
+}
+
 // The token at which the sums from `base` on pass the threshold, in the vectors g0 .. g1 - 1, by one warp: the first, else
-// (rounding) the last one with weight.  A lane looks at BATCH consecutive vectors, so that lane order is token order.
+// (rounding) the last one with weight.  A lane sums BATCH consecutive vectors, so that lane order is token order; then the lanes
+// take the entries of the lane that holds the crossing, one each.
 template <typename LT>
 __device__ __forceinline__ int find_token(const PairOfRows<LT> &r, bool pair, int g0, int g1, double base, double threshold)
 {
     constexpr int VEC = Logit<LT>::VEC;
+    static_assert(BATCH * VEC <= 32, "an entry per lane");
     const int lane = threadIdx.x & 31;
+    const LT *a = reinterpret_cast<const LT *>(r.a) + r.lead_a, *d = reinterpret_cast<const LT *>(r.d) + r.lead_d;
+    auto weight = [&](float p, float q, int v) {
+        if (!pair) q = v == r.certain ? 1.f : 0.f;
+        return p > q ? (double)p - (double)q : 0.0;
+    };
     int last = -1;
     for (int c = g0; c < g1; c += 32 * BATCH) {
-        uint4 ra[BATCH], rd[BATCH];
+        double mine = 0.0;
         const int g = c + lane * BATCH;
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
-            ra[i] = rd[i] = make_uint4(0u, 0u, 0u, 0u);
+            uint4 ra = make_uint4(0u, 0u, 0u, 0u), rd = ra;
             if (g + i < g1) {
-                ra[i] = vector_at<LT, true, true>(r.a, r.lead_a, g + i, r.V);
-                if (pair) rd[i] = vector_at<LT, true, true>(r.d, r.lead_d, g + i, r.V);
+                ra = vector_at<LT, true, true>(r.a, r.lead_a, g + i, r.V);
+                if (pair) rd = vector_at<LT, true, true>(r.d, r.lead_d, g + i, r.V);
             }
-        }
-        auto weight = [&](const float (&p)[VEC], const float (&q)[VEC], int i, int e) {
-            const float qe = pair ? q[e] : (g + i) * VEC + e == r.certain ? 1.f : 0.f;
-            return p[e] > qe ? (double)p[e] - (double)qe : 0.0;
-        };
-        double mine = 0.0;
-#pragma unroll
-        for (int i = 0; i < BATCH; ++i) {
             float p[VEC], q[VEC];
-            Logit<LT>::unpack(ra[i], p);
-            Logit<LT>::unpack(rd[i], q);
+            Logit<LT>::unpack(ra, p);
+            Logit<LT>::unpack(rd, q);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) mine += weight(p, q, i, e);
+            for (int e = 0; e < VEC; ++e) mine += weight(p[e], q[e], (g + i) * VEC + e);
         }
-        double upto = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const double t = __shfl_up_sync(FULL, upto, o);
-            if (lane >= o) upto += t;
-        }
-        const unsigned mass = __ballot_sync(FULL, mine > 0.0), hits = __ballot_sync(FULL, base + upto > threshold) & mass;
-        if (mass) {
-            const int src = hits ? __ffs(hits) - 1 : 31 - __clz(mass);
-            int found = -1;
-            if (lane == src) {
-                double run = base + (upto - mine);
-                bool done = false;
-#pragma unroll
-                for (int i = 0; i < BATCH; ++i) {
-                    float p[VEC], q[VEC];
-                    Logit<LT>::unpack(ra[i], p);
-                    Logit<LT>::unpack(rd[i], q);
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        const double w = weight(p, q, i, e);
-                        run += w;
-                        if (!done && w > 0.0) {
-                            found = (g + i) * VEC + e;
-                            done = run > threshold;
-                        }
-                    }
-                }
-            }
-            last = __shfl_sync(FULL, found, src);
-            if (hits) return last;
+        const double upto = lanes_up_to(mine);
+        bool beyond;
+        const int src = crossing_lane(mine, base + upto, threshold, beyond);
+        if (src >= 0) {
+            const int v = (c + src * BATCH) * VEC + lane;
+            double w = 0.0;
+            if (lane < BATCH * VEC && v < min(r.V, g1 * VEC)) w = weight(Logit<LT>::scalar_l2(a, v), pair ? Logit<LT>::scalar_l2(d, v) : 0.f, v);
+            bool any;
+            last = (c + src * BATCH) * VEC + crossing_lane(w, base + __shfl_sync(FULL, upto - mine, src) + lanes_up_to(w), threshold, any);
+            if (beyond) return last;
         }
         base += __shfl_sync(FULL, upto, 31);
     }
@@ -223,11 +287,11 @@ __device__ __forceinline__ int find_token(const PairOfRows<LT> &r, bool pair, in
 }
 
 template <typename LT, bool TV>
-__global__ void __launch_bounds__(PROBS_THREADS) probs_kernel(const ProbsParams p)
+__global__ void __launch_bounds__(PROBS_THREADS, 4) probs_kernel(const ProbsParams p)
 {
     constexpr int VEC = Logit<LT>::VEC;
     __shared__ double sh_weight[MAX_PARTS];     // the parts' sums; NaN: the part holds what is no probability
-    __shared__ float sh_apart[TV ? MAX_PARTS : 1];
+    __shared__ float sh_under[TV ? MAX_PARTS : 1];
     __shared__ int sh_n;
     __shared__ bool sh_again;
 
@@ -318,17 +382,17 @@ __global__ void __launch_bounds__(PROBS_THREADS) probs_kernel(const ProbsParams 
     else if (j < kb) r.certain = __ldg(tokens + j);
 
     const int parts = p.parts, part_vecs = p.part_vecs;
-    const uint32_t weights_at = map_to_rank(smem_addr(sh_weight), 0), apart_at = map_to_rank(smem_addr(sh_apart), 0);
+    const uint32_t weights_at = map_to_rank(smem_addr(sh_weight), 0), under_at = map_to_rank(smem_addr(sh_under), 0);
     bool published = false;
     for (int s = parts * rank / C + warp; s < parts * (rank + 1) / C; s += PROBS_WARPS) {
         const Sums x = sum_part<LT, TV>(r, pair, s * part_vecs, min((s + 1) * part_vecs, r.n_vec));
-        const double w = warp_sum(x.weight + (double)x.rest);
-        const float apart = TV ? warp_sum_f(x.apart) : 0.f;
+        const double w = warp_sum(weight_of(x));
+        const float under = TV ? warp_sum_f(sum2(x.under)) : 0.f;
         const bool bad = __any_sync(FULL, x.bad);
         if (!published) { cluster_wait(); published = true; }
         if (lane == 0) {
             st_cluster(weights_at + 8u * s, bad ? (double)NAN : w);
-            if (TV) st_cluster(apart_at + 4u * s, __float_as_int(apart));
+            if (TV) st_cluster(under_at + 4u * s, __float_as_int(under));
         }
     }
     if (!published) cluster_wait();
@@ -344,22 +408,17 @@ __global__ void __launch_bounds__(PROBS_THREADS) probs_kernel(const ProbsParams 
             double mine = 0.0;
             for (int i = 0; i < per; ++i)
                 if (lane * per + i < parts) mine += sh_weight[lane * per + i];
-            double upto = mine;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const double t = __shfl_up_sync(FULL, upto, o);
-                if (lane >= o) upto += t;
-            }
+            const double upto = lanes_up_to(mine);
             const double total = __shfl_sync(FULL, upto, 31);
             const bool bad = !(total < INFINITY);
             if (TV && first && j < kb) {
-                double apart = 0.0;
+                double under = 0.0;
                 for (int i = 0; i < per; ++i)
-                    if (lane * per + i < parts) apart += (double)sh_apart[lane * per + i];
-                apart = warp_sum(apart);
+                    if (lane * per + i < parts) under += (double)sh_under[lane * per + i];
+                under = warp_sum(under);
                 // a token outside the vocabulary has no place in the row
                 const bool nowhere = !pair && (r.certain < 0 || r.certain >= V);
-                if (lane == 0) p.d_tv[(int64_t)b * k + j] = bad || nowhere ? 1.f : (float)(0.5 * apart);
+                if (lane == 0) p.d_tv[(int64_t)b * k + j] = bad || nowhere ? 1.f : (float)(0.5 * (total + under));
                 if (bad) flags |= METASD_STATUS_NONFINITE;
             }
             if (draws) {
@@ -368,10 +427,8 @@ __global__ void __launch_bounds__(PROBS_THREADS) probs_kernel(const ProbsParams 
                     flags |= METASD_STATUS_NONFINITE;
                 } else if (total > 0.0) {
                     const double threshold = (double)__ldg(p.u_draw + b) * total;
-                    const int src = [&] {
-                        const unsigned mass = __ballot_sync(FULL, mine > 0.0), hits = __ballot_sync(FULL, upto > threshold) & mass;
-                        return hits ? __ffs(hits) - 1 : 31 - __clz(mass);
-                    }();
+                    bool beyond;
+                    const int src = crossing_lane(mine, upto, threshold, beyond);
                     int part = -1;
                     double base = 0.0;
                     if (lane == src) {
@@ -409,7 +466,7 @@ __global__ void __launch_bounds__(PROBS_THREADS) probs_kernel(const ProbsParams 
         pair = false;
         for (int s = warp; s < parts; s += PROBS_WARPS) {
             const Sums x = sum_part<LT, false>(r, false, s * part_vecs, min((s + 1) * part_vecs, r.n_vec));
-            const double w = warp_sum(x.weight + (double)x.rest);
+            const double w = warp_sum(weight_of(x));
             if (lane == 0) sh_weight[s] = w;
         }
         __syncthreads();
