@@ -185,66 +185,71 @@ class ProbsResult:
     reward: Optional[torch.Tensor] = None   # [B] fp32, of a context's round
 
 
-def _expect(name: str, t, dtype, shape, device: torch.device):
-    """The library sees addresses only: what they lead to is checked here."""
-    if t.dtype != dtype or tuple(t.shape) != shape or t.device != device or not t.is_contiguous():
-        raise ValueError("%s: a contiguous %s tensor of shape %s on %s is due, not %s of shape %s on %s" % (
-            name, dtype, shape, device, t.dtype, tuple(t.shape), t.device))
+def _refuse(name: str, t, dtype, shape, index: int):
+    raise ValueError("%s: a contiguous %s tensor of shape %s on cuda:%d is due, not %s" % (
+        name, dtype, tuple(shape), index, "%s of shape %s on %s" % (t.dtype, tuple(t.shape), t.device)
+        if isinstance(t, torch.Tensor) else type(t).__name__))
 
 
-def _strides(name: str, t, dtype, B: int, rows: int, V: int, device: torch.device):
-    """Strides of sequences and rows, in entries; rows may be apart, their entries may not."""
-    if t.dtype != dtype or t.shape != (B, rows, V) or t.device != device:
-        raise ValueError("%s: a %s tensor of shape %s on %s is due, not %s of shape %s on %s" % (
-            name, dtype, (B, rows, V), device, t.dtype, tuple(t.shape), t.device))
-    seq, row, entry = t.stride()
-    if entry != 1 and V > 1:
-        raise ValueError("%s: a row's entries have to lie next to each other (stride %d)" % (name, entry))
-    return seq, row
+# The library sees addresses only: what they lead to is checked here.  (dtypes are single objects; get_device() is -1 off CUDA)
+def _expect(name: str, t, dtype, shape, index: int):
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous()):
+        _refuse(name, t, dtype, shape, index)
 
 
 def _verify_probs(ctx, target, draft, tokens, u_accept, u_draw, draft_len, draft_place, seed, out, want_d_tv, status):
-    if not target.is_cuda or target.dim() != 3 or target.dtype not in (torch.bfloat16, torch.float32):
+    dtype, index = target.dtype, target.get_device()
+    if index < 0 or target.dim() != 3 or (dtype is not torch.float32 and dtype is not torch.bfloat16):
         raise ValueError("target_probs: a CUDA tensor [B, k + 1, V] of bf16 or fp32 is due")
-    dev = target.device
     B, rows, V = target.shape
-    k, i32, f32 = rows - 1, torch.int32, torch.float32
-    tss, trs = _strides("target_probs", target, target.dtype, B, rows, V, dev)
+    k, i32, f32, per_sequence = rows - 1, torch.int32, torch.float32, (B,)
+    tss, trs, entry = target.stride()
+    if entry != 1 and V > 1:
+        raise ValueError("target_probs: a row's entries have to lie next to each other (stride %d)" % entry)
     dss = drs = 0
-    if draft is not None:
-        dss, drs = _strides("draft_probs", draft, target.dtype, B, k, V, dev)
     if k > 0:
-        _expect("draft_tokens", tokens, i32, (B, k), dev)
-        _expect("u_accept", u_accept, f32, (B, k), dev)
+        drafted = (B, k)
+        if draft is not None:
+            if draft.dtype is not dtype or draft.shape != (B, k, V) or draft.get_device() != index:
+                _refuse("draft_probs", draft, dtype, (B, k, V), index)
+            dss, drs, entry = draft.stride()
+            if entry != 1 and V > 1:
+                raise ValueError("draft_probs: a row's entries have to lie next to each other (stride %d)" % entry)
+        _expect("draft_tokens", tokens, i32, drafted, index)
+        _expect("u_accept", u_accept, f32, drafted, index)
     else:
         tokens = u_accept = draft = None
-    _expect("u_draw", u_draw, f32, (B,), dev)
+    _expect("u_draw", u_draw, f32, per_sequence, index)
     if draft_len is not None:
-        _expect("draft_len", draft_len, i32, (B,), dev)
+        _expect("draft_len", draft_len, i32, per_sequence, index)
     if draft_place is not None:
-        _expect("draft_place", draft_place, i32, (B,), dev)
-    if status is not None and (status.dtype != i32 or status.device != dev or status.numel() < 1):
-        raise ValueError("status: an int32 tensor on %s is due" % dev)
+        _expect("draft_place", draft_place, i32, per_sequence, index)
+    if status is not None:
+        _expect("status", status, i32, (1,), index)
     if out is None:
-        out = ProbsResult(torch.empty(B, dtype=i32, device=dev), torch.empty(B, dtype=i32, device=dev))
+        out = ProbsResult(torch.empty_like(u_draw, dtype=i32), torch.empty_like(u_draw, dtype=i32))
     else:
-        _expect("accepted_len", out.accepted_len, i32, (B,), dev)
-        _expect("next_token", out.next_token, i32, (B,), dev)
-    if want_d_tv and out.d_tv is None:
-        out.d_tv = torch.zeros((B, k), dtype=f32, device=dev)
-    elif want_d_tv:
-        _expect("d_tv", out.d_tv, f32, (B, k), dev)
-    d_tv = out.d_tv if want_d_tv and k > 0 else None
+        _expect("accepted_len", out.accepted_len, i32, per_sequence, index)
+        _expect("next_token", out.next_token, i32, per_sequence, index)
+    d_tv = None
+    if want_d_tv:
+        if out.d_tv is None:
+            out.d_tv = torch.zeros((B, k), dtype=f32, device=target.device)
+        else:
+            _expect("d_tv", out.d_tv, f32, (B, k), index)
+        if k > 0:
+            d_tv = out.d_tv
     reward = None
     if ctx is not None:
         if out.reward is None:
-            out.reward = torch.empty(B, dtype=f32, device=dev)
+            out.reward = torch.empty_like(u_draw)
         else:
-            _expect("reward", out.reward, f32, (B,), dev)
+            _expect("reward", out.reward, f32, per_sequence, index)
         reward = out.reward
     lib = _lib or load_library()
-    args = (ctx, dev.index, B, k, V, DTYPES[target.dtype], target, tss, trs, draft, dss, drs, draft_place, tokens, draft_len, u_accept,
-            u_draw, seed, out.accepted_len, out.next_token, d_tv, reward, status, _stream(dev))
+    stream = _raw_stream(index) if _raw_stream is not None else _stream(target.device)
+    args = (ctx, index, B, k, V, BF16 if dtype is torch.bfloat16 else FP32, target, tss, trs, draft, dss, drs, draft_place, tokens, draft_len,
+            u_accept, u_draw, seed, out.accepted_len, out.next_token, d_tv, reward, status, stream)
     rc = NotImplemented
     if _call is not None:
         rc = _call.verify_probs(lib.verify_probs_at, *args)
@@ -461,20 +466,20 @@ class BlockCache:
             raise ValueError("block_table [n_pools, max_batch, max_blocks] and free_blocks [n_pools, n_blocks] are due, on a CUDA device")
         P, B, M = block_table.shape
         dev, i32 = block_table.device, torch.int32
-        _expect("block_table", block_table, i32, (P, B, M), dev)
-        _expect("held", held, i32, (P, B), dev)
-        _expect("free_blocks", free_blocks, i32, (P, free_blocks.shape[1]), dev)
-        _expect("free_count", free_count, i32, (P,), dev)
+        _expect("block_table", block_table, i32, (P, B, M), dev.index)
+        _expect("held", held, i32, (P, B), dev.index)
+        _expect("free_blocks", free_blocks, i32, (P, free_blocks.shape[1]), dev.index)
+        _expect("free_count", free_count, i32, (P,), dev.index)
         if status is None:
             status = torch.zeros(1, dtype=i32, device=dev)
-        _expect("status", status, i32, (1,), dev)
+        _expect("status", status, i32, (1,), dev.index)
         self.lib = load_library()
         n = self.lib.metasd_cache_workspace_bytes(B, P)
         if n == 0 or page_size < 1:
             raise MetasdError(ERR_INVALID_ARGUMENT, "metasd_cache_workspace_bytes")
         self.block_table, self.held, self.free_blocks, self.free_count, self.status = block_table, held, free_blocks, free_count, status
         self.workspace = torch.empty(n, dtype=torch.uint8, device=dev)
-        self.device, self.n_pools, self.max_batch, self.page_size = dev, P, B, int(page_size)
+        self.device, self.index, self.n_pools, self.max_batch, self.page_size = dev, dev.index, P, B, int(page_size)
         self._c = MetasdCache(*[t.data_ptr() for t in (block_table, held, free_blocks, free_count, self.workspace, status)],
                               P, B, M, free_blocks.shape[1], self.page_size, dev.index)
         self._at = C.addressof(self._c)
@@ -490,39 +495,53 @@ class BlockCache:
 
     def _per_pool(self, name: str, t: torch.Tensor, B: int) -> int:
         """Entries between pools: of a [B] tensor (the same for all) or an [n_pools, B] one."""
-        _expect(name, t, torch.int32, (B,) if t.dim() == 1 else (self.n_pools, B), self.device)
-        return 0 if t.dim() == 1 else B
+        if t.dim() == 1:
+            _expect(name, t, torch.int32, (B,), self.index)
+            return 0
+        _expect(name, t, torch.int32, (self.n_pools, B), self.index)
+        return B
+
+    def _stream(self) -> int:
+        return _raw_stream(self.index) if _raw_stream is not None else _stream(self.device)
 
     def plan(self, length: torch.Tensor, cached: torch.Tensor, pool: Optional[torch.Tensor] = None,
              max_tokens: Optional[int] = None, out: Optional[CachePlan] = None) -> CachePlan:
         """metasd_cache_plan: length [B], cached [B] or [n_pools, B], pool [B] (None: pool 0), int32.  max_tokens: entries that the
         outputs have room for, where they are not given."""
-        dev, i32 = self.device, torch.int32
+        index, i32 = self.index, torch.int32
         B = length.shape[0]
-        _expect("length", length, i32, (B,), dev)
+        each = (B,)
+        _expect("length", length, i32, each, index)
         stride = self._per_pool("cached", cached, B)
         if pool is not None:
-            _expect("pool", pool, i32, (B,), dev)
+            _expect("pool", pool, i32, each, index)
         if out is None:
             if max_tokens is None:
                 raise ValueError("max_tokens or the outputs are due")
             def ints(*shape):
-                return torch.empty(shape, dtype=i32, device=dev)
+                return torch.empty(shape, dtype=i32, device=self.device)
             out = CachePlan(ints(B), ints(B), ints(self.n_pools + 1), ints(B + 1),
-                            torch.empty(max_tokens, dtype=torch.int64, device=dev), ints(max_tokens), ints(max_tokens))
+                            torch.empty(max_tokens, dtype=torch.int64, device=self.device), ints(max_tokens), ints(max_tokens))
         else:
-            room = out.slot_map.shape[0]
+            slot_map = out.slot_map
+            room = slot_map.shape[0]
             if max_tokens is not None and max_tokens != room:
                 raise ValueError("slot_map has room for %d entries, not %d" % (room, max_tokens))
             max_tokens = room
-            _expect("slot_map", out.slot_map, torch.int64, (room,), dev)
-            _expect("token_start", out.token_start, i32, (B + 1,), dev)
-            for name, t, shape in (("order", out.order, (B,)), ("place", out.place, (B,)), ("pool_start", out.pool_start, (self.n_pools + 1,)),
-                                   ("position", out.position, (room,)), ("sequence", out.sequence, (room,))):
-                if t is not None:
-                    _expect(name, t, i32, shape, dev)
+            _expect("slot_map", slot_map, torch.int64, (room,), index)
+            _expect("token_start", out.token_start, i32, (B + 1,), index)
+            if out.order is not None:
+                _expect("order", out.order, i32, each, index)
+            if out.place is not None:
+                _expect("place", out.place, i32, each, index)
+            if out.pool_start is not None:
+                _expect("pool_start", out.pool_start, i32, (self.n_pools + 1,), index)
+            if out.position is not None:
+                _expect("position", out.position, i32, (room,), index)
+            if out.sequence is not None:
+                _expect("sequence", out.sequence, i32, (room,), index)
         args = (self._at, B, pool, cached, stride, length, max_tokens, out.order, out.place, out.pool_start, out.token_start, out.slot_map,
-                out.position, out.sequence, _stream(dev))
+                out.position, out.sequence, self._stream())
         rc = NotImplemented
         if _call is not None:
             rc = _call.cache_plan(self.lib.cache_plan_at, *args)
@@ -535,8 +554,7 @@ class BlockCache:
     def release(self, keep: torch.Tensor):
         """metasd_cache_release: keep [B] (all pools) or [n_pools, B] int32, the entries that stay."""
         B = keep.shape[-1]
-        stride = self._per_pool("keep", keep, B)
-        args = (self._at, B, keep, stride, _stream(self.device))
+        args = (self._at, B, keep, self._per_pool("keep", keep, B), self._stream())
         rc = NotImplemented
         if _call is not None:
             rc = _call.cache_release(self.lib.cache_release_at, *args)

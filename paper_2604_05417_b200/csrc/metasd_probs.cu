@@ -21,7 +21,7 @@ namespace metasd {
 
 namespace {
 
-constexpr int PROBS_THREADS = 256, PROBS_WARPS = PROBS_THREADS / 32;
+constexpr int THREADS = 256, WARPS = THREADS / 32;
 constexpr int MAX_PARTS = 256;      // of a row; 8 per lane of the warp that looks for the crossing
 constexpr int BATCH = 4;            // vectors of a row that a lane has in flight
 constexpr unsigned FULL = 0xFFFFFFFFu;
@@ -57,18 +57,18 @@ template <typename LT> __device__ __forceinline__ uint4 cut(uint4 v, int n)
 }
 
 // Vector g of a row that starts `lead` entries behind a 16-byte boundary.  No 16 bytes are read that hold nothing of the row.
-template <typename LT, bool SHIFTED, bool AGAIN> __device__ __forceinline__ uint4 vector_at(const uint4 *row, int lead, int g, int V)
+template <typename LT, bool SHIFTED> __device__ __forceinline__ uint4 vector_at(const uint4 *row, int lead, int g, int V)
 {
     constexpr int VEC = Logit<LT>::VEC;
     const int n = V - g * VEC;      // entries from here to the row's end
     uint4 v;
     if (!SHIFTED) {
-        v = AGAIN ? __ldcg(row + g) : ld_stream(row + g);
+        v = ld_stream(row + g);
     } else {
-        v = AGAIN ? __ldcg(row + g) : __ldg(row + g);
+        v = __ldg(row + g);
         if (lead) {
             uint4 next = make_uint4(0u, 0u, 0u, 0u);
-            if (lead + min(n, VEC) > VEC) next = AGAIN ? __ldcg(row + g + 1) : __ldg(row + g + 1);
+            if (lead + min(n, VEC) > VEC) next = __ldg(row + g + 1);
             v = Logit<LT>::shifted(v, next, lead);
         }
     }
@@ -117,16 +117,21 @@ template <typename LT> __device__ __forceinline__ uint64_t pair_at(const uint4 &
     else return pack2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
 }
 
-// A pair of entries of both rows.  With m = max(p, q), m - q is max(0, p - q) with no comparison of its own.
-template <bool TV> __device__ __forceinline__ void add_pair(Sums &s, uint64_t p, uint64_t q)
+// A pair of entries of both rows.  With m = max(p, q), m - q is max(0, p - q) with no comparison of its own.  `over` goes through
+// the same roundings whether what they take away is kept (EXACT: the row may be drawn from) or not.
+template <bool EXACT, bool TV> __device__ __forceinline__ void add_pair(Sums &s, uint64_t p, uint64_t q)
 {
     const uint64_t m = max2(p, q), d = sub2(m, q);
-    s.rest = add2(s.rest, sub2(sub2(m, d), q));
-    add_exactly(s.over, s.rest, d);
+    if (EXACT) {
+        s.rest = add2(s.rest, sub2(sub2(m, d), q));
+        add_exactly(s.over, s.rest, d);
+    } else {
+        s.over = add2(s.over, d);
+    }
     if (TV) s.under = add2(s.under, sub2(m, p));
 }
 
-template <typename LT, bool PAIR, bool TV>
+template <typename LT, bool PAIR, bool EXACT, bool TV>
 __device__ __forceinline__ void add_vectors(Sums &s, const uint4 &ra, const uint4 &rd, int tok0, int certain)
 {
     constexpr int VEC = Logit<LT>::VEC;
@@ -140,14 +145,17 @@ __device__ __forceinline__ void add_vectors(Sums &s, const uint4 &ra, const uint
     }
     if (PAIR) {
 #pragma unroll
-        for (int i = 0; i < VEC / 2; ++i) add_pair<TV>(s, pair_at<LT>(ra, i), pair_at<LT>(rd, i));
+        for (int i = 0; i < VEC / 2; ++i) add_pair<EXACT, TV>(s, pair_at<LT>(ra, i), pair_at<LT>(rd, i));
     } else if (certain < tok0 || certain >= tok0 + VEC) {
 #pragma unroll
-        for (int i = 0; i < VEC / 2; ++i) add_exactly(s.over, s.rest, pair_at<LT>(ra, i));
+        for (int i = 0; i < VEC / 2; ++i) {
+            if (EXACT) add_exactly(s.over, s.rest, pair_at<LT>(ra, i));
+            else s.over = add2(s.over, pair_at<LT>(ra, i));
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < VEC / 2; ++i)
-            add_pair<TV>(s, pair_at<LT>(ra, i), pack2(certain == tok0 + 2 * i ? 1.f : 0.f, certain == tok0 + 2 * i + 1 ? 1.f : 0.f));
+            add_pair<EXACT, TV>(s, pair_at<LT>(ra, i), pack2(certain == tok0 + 2 * i ? 1.f : 0.f, certain == tok0 + 2 * i + 1 ? 1.f : 0.f));
     }
 }
 
@@ -160,63 +168,128 @@ __device__ __forceinline__ double weight_of(const Sums &s)
     return (double)sum + (double)(((lo - (sum - part)) + (hi - part)) + sum2(s.rest));
 }
 
-// The sums of the vectors g0 .. g1 - 1 (a multiple of 32 from g0), a lane every 32nd.  The order of additions does not depend on where the rows
-// start: off 16-byte boundaries a vector is two loads (the second one's line is in L1), so that half as many are in flight.
-template <typename LT, bool PAIR, bool TV, bool SHIFTED>
-__device__ __forceinline__ Sums sum_part(const PairOfRows<LT> &r, int g0, int g1)
+// A warp's BATCH vectors of 32 lanes, read from 16-byte boundaries LEAD entries in front of the row's, become the row's: what a
+// lane lacks, the next one has (the last lane: the first, of the next vector; `behind` follows the last vector).
+template <typename LT, int LEAD> __device__ __forceinline__ void realign(uint4 (&v)[BATCH], const uint4 &behind)
 {
-    constexpr int VEC = Logit<LT>::VEC, N = SHIFTED ? BATCH / 2 : BATCH;
-    Sums s = {0ull, 0ull, 0ull, false};
-    int g = g0 + (threadIdx.x & 31);
-    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-    // whole vectors, whole batches: nothing but loads and sums
-    for (int c = g0; c + 32 * N <= min(g1, r.V / VEC); c += 32 * N, g += 32 * N) {
-        uint4 ra[N], rd[N];
-        if (!SHIFTED) {
+    constexpr bool HALF = sizeof(LT) == 2 && LEAD % 2 != 0;
+    constexpr int WORDS = sizeof(LT) == 2 ? LEAD / 2 : LEAD, MORE = WORDS + HALF;   // whole words to skip; words of the next lane
+    const int lane = threadIdx.x & 31;
 #pragma unroll
-            for (int i = 0; i < N; ++i) ra[i] = ld_stream(r.a + g + 32 * i);
-            if (PAIR) {
+    for (int i = 0; i < BATCH; ++i) {
+        const uint4 n = i + 1 < BATCH ? v[i + 1 < BATCH ? i + 1 : 0] : behind;
+        uint32_t w[8] = {v[i].x, v[i].y, v[i].z, v[i].w, n.x, n.y, n.z, n.w};
 #pragma unroll
-                for (int i = 0; i < N; ++i) rd[i] = ld_stream(r.d + g + 32 * i);
-            }
-        } else {
-            uint4 na[N], nd[N];
+        for (int j = 0; j < MORE; ++j) w[4 + j] = __shfl_sync(FULL, lane == 0 ? w[4 + j] : w[j], (lane + 1) & 31);
+        uint32_t o[4];
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                ra[i] = __ldg(r.a + g + 32 * i);
-                na[i] = r.lead_a ? __ldg(r.a + g + 32 * i + 1) : zero;
-            }
-            if (PAIR) {
-#pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    rd[i] = __ldg(r.d + g + 32 * i);
-                    nd[i] = r.lead_d ? __ldg(r.d + g + 32 * i + 1) : zero;
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                ra[i] = Logit<LT>::shifted(ra[i], na[i], r.lead_a);
-                if (PAIR) rd[i] = Logit<LT>::shifted(rd[i], nd[i], r.lead_d);
+        for (int j = 0; j < 4; ++j) o[j] = HALF ? __byte_perm(w[j + WORDS], w[(j + WORDS + 1) & 7], 0x5432) : w[j + WORDS];
+        v[i] = make_uint4(o[0], o[1], o[2], o[3]);
+    }
+}
+template <typename LT> __device__ __forceinline__ void realign(uint4 (&v)[BATCH], const uint4 &behind, int lead)
+{
+    switch (lead) {
+    case 1: realign<LT, 1>(v, behind); break;
+    case 2: realign<LT, 2>(v, behind); break;
+    case 3: realign<LT, 3>(v, behind); break;
+    default:
+        if constexpr (sizeof(LT) == 2) {
+            switch (lead) {
+            case 4: realign<LT, 4>(v, behind); break;
+            case 5: realign<LT, 5>(v, behind); break;
+            case 6: realign<LT, 6>(v, behind); break;
+            case 7: realign<LT, 7>(v, behind); break;
             }
         }
-#pragma unroll
-        for (int i = 0; i < N; ++i) add_vectors<LT, PAIR, TV>(s, ra[i], PAIR ? rd[i] : zero, (g + 32 * i) * VEC, r.certain);
     }
-    // the row's end
-#pragma unroll 1
-    for (; g < g1; g += 32) {
-        const uint4 ra = vector_at<LT, SHIFTED, false>(r.a, r.lead_a, g, r.V);
-        const uint4 rd = PAIR ? vector_at<LT, SHIFTED, false>(r.d, r.lead_d, g, r.V) : zero;
-        add_vectors<LT, PAIR, TV>(s, ra, rd, g * VEC, r.certain);
-    }
-    return s;
 }
 
-template <typename LT, bool TV>
-__device__ __forceinline__ Sums sum_part(const PairOfRows<LT> &r, bool pair, int g0, int g1)
+// 32 BATCH vectors of a row from vector c on, all of them whole.
+template <typename LT, bool SHIFTED> __device__ __forceinline__ void load_batch(uint4 (&v)[BATCH], const uint4 *row, int lead, int c)
 {
-    if (pair) return (r.lead_a | r.lead_d) == 0 ? sum_part<LT, true, TV, false>(r, g0, g1) : sum_part<LT, true, TV, true>(r, g0, g1);
-    return r.lead_a == 0 ? sum_part<LT, false, TV, false>(r, g0, g1) : sum_part<LT, false, TV, true>(r, g0, g1);
+    const uint4 *at = row + c + (threadIdx.x & 31);
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) v[i] = ld_stream(at + 32 * i);
+}
+template <typename LT, bool SHIFTED> __device__ __forceinline__ uint4 load_behind(const uint4 *row, int lead, int c)
+{
+    return SHIFTED && lead ? ld_stream(row + c + 32 * BATCH) : make_uint4(0u, 0u, 0u, 0u);
+}
+
+template <typename LT, bool PAIR, bool EXACT, bool TV>
+__device__ __forceinline__ void add_batch(Sums &s, const uint4 (&ra)[BATCH], const uint4 (&rd)[BATCH], int c, int certain)
+{
+    constexpr int VEC = Logit<LT>::VEC;
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) add_vectors<LT, PAIR, EXACT, TV>(s, ra[i], rd[i], (c + 32 * i + (int)(threadIdx.x & 31)) * VEC, certain);
+}
+
+// A warp's sums of a part, put where the sequence's sums are collected.
+template <bool EXACT, bool TV> __device__ __forceinline__ void publish(const Sums &x, int s, uint32_t weights_at, uint32_t apart_at)
+{
+    const double w = EXACT ? warp_sum(weight_of(x)) : 0.0;
+    const float apart = TV ? warp_sum_f(sum2(add2(x.over, x.under))) : 0.f;
+    const bool bad = __any_sync(FULL, x.bad);
+    if ((threadIdx.x & 31) == 0) {
+        st_cluster(weights_at + 8u * s, bad ? (double)NAN : w);
+        if (TV) st_cluster(apart_at + 4u * s, __float_as_int(apart));
+    }
+}
+
+// The parts s0, s0 + step, .. below s1 of a row (pair), by one warp.  The order of additions does not depend on where the rows
+// start, and keeping what the roundings take away (EXACT) does not change the other sums.
+// Asks L2 for a batch: 2 KB of each row, a line per lane.
+template <typename LT> __device__ __forceinline__ void prefetch_batch(const PairOfRows<LT> &r, bool pair, int c)
+{
+    const int lane = threadIdx.x & 31, g = c + 8 * (lane & 15);
+    const uint4 *row = lane < 16 ? r.a : r.d;
+    if ((lane < 16 || pair) && g < r.n_vec) asm volatile("prefetch.global.L2 [%0];" ::"l"(row + g));
+}
+
+template <typename LT, bool PAIR, bool EXACT, bool TV, bool SHIFTED>
+__device__ __forceinline__ void sum_parts(const PairOfRows<LT> r, int part_vecs, int s0, int s1, int step, uint32_t weights_at, uint32_t apart_at)
+{
+    constexpr int VEC = Logit<LT>::VEC;
+    const int whole = r.V / VEC;
+    for (int s = s0; s < s1; s += step) {
+        const int g0 = s * part_vecs, g1 = min(g0 + part_vecs, r.n_vec);
+        Sums x = {0ull, 0ull, 0ull, false};
+        int c = g0;
+        // whole vectors, whole batches: nothing but loads and sums
+        for (; c + 32 * BATCH <= min(g1, whole); c += 32 * BATCH) {
+            uint4 ra[BATCH], rd[BATCH];
+            load_batch<LT, SHIFTED>(ra, r.a, r.lead_a, c);
+            const uint4 behind_a = load_behind<LT, SHIFTED>(r.a, r.lead_a, c);
+            if (PAIR) {
+                load_batch<LT, SHIFTED>(rd, r.d, r.lead_d, c);
+                const uint4 behind_d = load_behind<LT, SHIFTED>(r.d, r.lead_d, c);
+                if (SHIFTED) realign<LT>(rd, behind_d, r.lead_d);
+            }
+            if (SHIFTED) realign<LT>(ra, behind_a, r.lead_a);
+            add_batch<LT, PAIR, EXACT, TV>(x, ra, PAIR ? rd : ra, c, r.certain);
+        }
+        // the row's end
+#pragma unroll 1
+        for (int g = c + (threadIdx.x & 31); g < g1; g += 32) {
+            const uint4 ra = vector_at<LT, SHIFTED>(r.a, r.lead_a, g, r.V);
+            const uint4 rd = PAIR ? vector_at<LT, SHIFTED>(r.d, r.lead_d, g, r.V) : ra;
+            add_vectors<LT, PAIR, EXACT, TV>(x, ra, rd, g * VEC, r.certain);
+        }
+        publish<EXACT, TV>(x, s, weights_at, apart_at);
+    }
+}
+
+template <typename LT, bool EXACT, bool TV>
+__device__ __forceinline__ void sum_parts(const PairOfRows<LT> &r, bool pair, int part_vecs, int s0, int s1, int step, uint32_t weights_at, uint32_t apart_at)
+{
+    if (pair) {
+        if ((r.lead_a | r.lead_d) == 0) sum_parts<LT, true, EXACT, TV, false>(r, part_vecs, s0, s1, step, weights_at, apart_at);
+        else sum_parts<LT, true, EXACT, TV, true>(r, part_vecs, s0, s1, step, weights_at, apart_at);
+    } else {
+        if (r.lead_a == 0) sum_parts<LT, false, EXACT, TV, false>(r, part_vecs, s0, s1, step, weights_at, apart_at);
+        else sum_parts<LT, false, EXACT, TV, true>(r, part_vecs, s0, s1, step, weights_at, apart_at);
+    }
 }
 
 // Inclusive sums over the lanes.
@@ -239,61 +312,83 @@ __device__ __forceinline__ int crossing_lane(double x, double upto, double thres
     return hits ? __ffs(hits) - 1 : 31 - __clz(mass);
 }
 
-// The token at which the sums from `base` on pass the threshold, in the vectors g0 .. g1 - 1, by one warp: the first, else
-// (rounding) the last one with weight.  A lane sums BATCH consecutive vectors, so that lane order is token order; then the lanes
-// take the entries of the lane that holds the crossing, one each.
+// What the block looks for in a part of a row: the token at which the sums from `base` on pass the threshold.
+struct Crossing {
+    double base, threshold;
+    int g0, g1;         // the part's vectors
+    int last;           // the last token with weight so far, for sums that rounding leaves below the threshold
+    bool again;         // nothing is left over of the target's row: it is drawn from as it stands
+};
+
+// By all threads, a vector each and a stretch of THREADS vectors at a time; returns to one thread the token, to the others -1.  A thread's
+// sums end, bit for bit, where the next one's begin: one of them holds the threshold, or none.
 template <typename LT>
-__device__ __forceinline__ int find_token(const PairOfRows<LT> &r, bool pair, int g0, int g1, double base, double threshold)
+__device__ __forceinline__ int find_token(const PairOfRows<LT> &r, bool pair, Crossing &sh, double (&sh_warp)[WARPS])
 {
     constexpr int VEC = Logit<LT>::VEC;
-    static_assert(BATCH * VEC <= 32, "an entry per lane");
-    const int lane = threadIdx.x & 31;
-    const LT *a = reinterpret_cast<const LT *>(r.a) + r.lead_a, *d = reinterpret_cast<const LT *>(r.d) + r.lead_d;
-    auto weight = [&](float p, float q, int v) {
-        if (!pair) q = v == r.certain ? 1.f : 0.f;
-        return p > q ? (double)p - (double)q : 0.0;
-    };
-    int last = -1;
-    for (int c = g0; c < g1; c += 32 * BATCH) {
-        double mine = 0.0;
-        const int g = c + lane * BATCH;
-#pragma unroll
-        for (int i = 0; i < BATCH; ++i) {
-            uint4 ra = make_uint4(0u, 0u, 0u, 0u), rd = ra;
-            if (g + i < g1) {
-                ra = vector_at<LT, true, true>(r.a, r.lead_a, g + i, r.V);
-                if (pair) rd = vector_at<LT, true, true>(r.d, r.lead_d, g + i, r.V);
-            }
-            float p[VEC], q[VEC];
-            Logit<LT>::unpack(ra, p);
-            Logit<LT>::unpack(rd, q);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) mine += weight(p[e], q[e], (g + i) * VEC + e);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    double base = sh.base;
+    const double threshold = sh.threshold;
+    for (int c = sh.g0; c < sh.g1; c += THREADS) {
+        const int g = c + tid;
+        uint4 ra = make_uint4(0u, 0u, 0u, 0u), rd = ra;
+        if (g < sh.g1) {
+            ra = vector_at<LT, true>(r.a, r.lead_a, g, r.V);
+            if (pair) rd = vector_at<LT, true>(r.d, r.lead_d, g, r.V);
         }
+        float p[VEC], q[VEC];
+        Logit<LT>::unpack(ra, p);
+        Logit<LT>::unpack(rd, q);
+        double w[VEC], mine = 0.0;
+        int last = -1;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            if (!pair) q[e] = g * VEC + e == r.certain ? 1.f : 0.f;
+            w[e] = p[e] > q[e] ? (double)p[e] - (double)q[e] : 0.0;
+            if (w[e] > 0.0) last = g * VEC + e;
+        }
+#pragma unroll
+        for (int e = 0; e < VEC; e += 2) mine += w[e] + w[e + 1];
         const double upto = lanes_up_to(mine);
-        bool beyond;
-        const int src = crossing_lane(mine, base + upto, threshold, beyond);
-        if (src >= 0) {
-            const int v = (c + src * BATCH) * VEC + lane;
-            double w = 0.0;
-            if (lane < BATCH * VEC && v < min(r.V, g1 * VEC)) w = weight(Logit<LT>::scalar_l2(a, v), pair ? Logit<LT>::scalar_l2(d, v) : 0.f, v);
-            bool any;
-            last = (c + src * BATCH) * VEC + crossing_lane(w, base + __shfl_sync(FULL, upto - mine, src) + lanes_up_to(w), threshold, any);
-            if (beyond) return last;
+        double start = __shfl_up_sync(FULL, upto, 1);
+        if (lane == 0) start = 0.0;
+        if (lane == 31) sh_warp[warp] = upto;
+        last = __reduce_max_sync(FULL, last);
+        if (lane == 0 && last >= 0) atomicMax(&sh.last, last);
+        __syncthreads();
+        double offset = base;
+        for (int i = 0; i < warp; ++i) offset += sh_warp[i];
+        double end = offset;
+        for (int i = warp; i < WARPS; ++i) end += sh_warp[i];
+        const bool mass = mine > 0.0, here = mass && offset + start <= threshold && offset + upto > threshold;
+        int token = -1;
+        if (here) {
+            double run = offset + start;
+            bool done = false;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                run += w[e];
+                if (!done && w[e] > 0.0) {
+                    token = g * VEC + e;
+                    done = run > threshold;
+                }
+            }
         }
-        base += __shfl_sync(FULL, upto, 31);
+        if (__syncthreads_or(here)) return token;
+        base = end;
     }
-    return last;
+    return tid == 0 ? sh.last : -1;
 }
 
 template <typename LT, bool TV>
-__global__ void __launch_bounds__(PROBS_THREADS, 4) probs_kernel(const ProbsParams p)
+__global__ void __launch_bounds__(THREADS, 4) probs_kernel(const ProbsParams p)
 {
     constexpr int VEC = Logit<LT>::VEC;
     __shared__ double sh_weight[MAX_PARTS];     // the parts' sums; NaN: the part holds what is no probability
-    __shared__ float sh_under[TV ? MAX_PARTS : 1];
-    __shared__ int sh_n;
-    __shared__ bool sh_again;
+    __shared__ float sh_apart[TV ? MAX_PARTS : 1];
+    __shared__ int sh_n, sh_token;
+    __shared__ Crossing sh_crossing;
+    __shared__ double sh_warp[WARPS];
 
     launch_dependents();
     grid_dependency_wait();
@@ -331,13 +426,33 @@ __global__ void __launch_bounds__(PROBS_THREADS, 4) probs_kernel(const ProbsPara
         return;
     }
 
-    // The accept tests, a lane each, by one warp.
+    const int parts = p.parts, part_vecs = p.part_vecs, s0 = parts * rank / C + warp, s1 = parts * (rank + 1) / C;
     const int32_t *tokens = p.tokens + (int64_t)b * k;
-    auto first_rejection = [&]() {
+    PairOfRows<LT> r;
+    bool pair = false;
+    auto rows_of = [&](int position) {
+        r.a = vectors_of(target + position * p.target_row, r.lead_a);
+        pair = draft && position < kb;
+        r.d = r.a;
+        r.lead_d = 0;
+        if (pair) r.d = vectors_of(draft + position * p.draft_row, r.lead_d);
+    };
+    r.V = V;
+    r.n_vec = (V + VEC - 1) / VEC;
+    r.certain = -1;
+    if (TV && j < kb) {     // this row is read whatever the tests say: its first lines come meanwhile
+        rows_of(j);
+        if (!draft) r.certain = __ldg(tokens + j);
+        if (s0 < s1) prefetch_batch(r, pair, s0 * part_vecs);
+    }
+    const float u_draw = rank == 0 && warp == 0 ? __ldg(p.u_draw + b) : 0.f;
+    // The accept tests, a lane each, by one warp.
+    if (warp == 0) {
         bool accepted = false;
         uint32_t f = 0;
+        int x = -1;
         if (lane < kb) {
-            const int x = __ldg(tokens + lane);
+            x = __ldg(tokens + lane);
             const float u = __ldg(p.u_accept + (int64_t)b * k + lane);
             if (x < 0 || x >= V) {
                 f |= METASD_STATUS_TOKEN_OOR;
@@ -353,124 +468,98 @@ __global__ void __launch_bounds__(PROBS_THREADS, 4) probs_kernel(const ProbsPara
             }
         }
         flags |= __reduce_or_sync(FULL, f);
-        return __ffs(__ballot_sync(FULL, !accepted)) - 1;   // lanes from kb on never accept
-    };
-    int n = -1;
+        const int stop = __ffs(__ballot_sync(FULL, !accepted)) - 1;     // lanes from kb on never accept
+        if (lane == stop) { sh_n = stop; sh_token = x; }
+    }
+    __syncthreads();
+    const int n = sh_n;
+    if (TV && j == kb && n < kb) return;       // no bonus token
     if (!TV || j == kb) {
-        if (warp == 0) {
-            n = first_rejection();
-            if (lane == 0) sh_n = n;
-        }
-        __syncthreads();
-        n = sh_n;
-        if (TV && n < kb) return;       // no bonus token
         j = n;
-    } else if (rank == 0 && warp == 0) {
-        n = first_rejection();
+        rows_of(j);
+        if (!TV && !draft && j < kb) r.certain = sh_token;
     }
     cluster_arrive_relaxed();           // every CTA of the cluster runs: its shared memory may be written
 
-    PairOfRows<LT> r;
-    r.V = V;
-    r.n_vec = (V + VEC - 1) / VEC;
-    r.a = vectors_of(target + j * p.target_row, r.lead_a);
-    bool pair = draft && j < kb;
-    r.d = r.a;
-    r.lead_d = 0;
-    r.certain = -1;
-    if (pair) r.d = vectors_of(draft + j * p.draft_row, r.lead_d);
-    else if (j < kb) r.certain = __ldg(tokens + j);
-
-    const int parts = p.parts, part_vecs = p.part_vecs;
-    const uint32_t weights_at = map_to_rank(smem_addr(sh_weight), 0), under_at = map_to_rank(smem_addr(sh_under), 0);
-    bool published = false;
-    for (int s = parts * rank / C + warp; s < parts * (rank + 1) / C; s += PROBS_WARPS) {
-        const Sums x = sum_part<LT, TV>(r, pair, s * part_vecs, min((s + 1) * part_vecs, r.n_vec));
-        const double w = warp_sum(weight_of(x));
-        const float under = TV ? warp_sum_f(sum2(x.under)) : 0.f;
-        const bool bad = __any_sync(FULL, x.bad);
-        if (!published) { cluster_wait(); published = true; }
-        if (lane == 0) {
-            st_cluster(weights_at + 8u * s, bad ? (double)NAN : w);
-            if (TV) st_cluster(under_at + 4u * s, __float_as_int(under));
-        }
-    }
-    if (!published) cluster_wait();
+    const uint32_t weights_at = map_to_rank(smem_addr(sh_weight), 0), apart_at = map_to_rank(smem_addr(sh_apart), 0);
+    cluster_wait();
+    if (!TV || n == j) sum_parts<LT, true, TV>(r, pair, part_vecs, s0, s1, WARPS, weights_at, apart_at);
+    else if constexpr (TV) sum_parts<LT, false, true>(r, pair, part_vecs, s0, s1, WARPS, weights_at, apart_at);
     cluster_sync_all();
     if (rank != 0) return;
 
     // One warp puts the parts together: lane l holds parts l per .. l per + per - 1.
+    constexpr int PER = MAX_PARTS / 32;
     const int per = (parts + 31) / 32;
-    const bool draws = n == j;      // warp 0 knows n
     for (bool first = true;; first = false) {
-        bool again = false;
         if (warp == 0) {
-            double mine = 0.0;
-            for (int i = 0; i < per; ++i)
-                if (lane * per + i < parts) mine += sh_weight[lane * per + i];
-            const double upto = lanes_up_to(mine);
-            const double total = __shfl_sync(FULL, upto, 31);
-            const bool bad = !(total < INFINITY);
-            if (TV && first && j < kb) {
-                double under = 0.0;
-                for (int i = 0; i < per; ++i)
-                    if (lane * per + i < parts) under += (double)sh_under[lane * per + i];
-                under = warp_sum(under);
-                // a token outside the vocabulary has no place in the row
-                const bool nowhere = !pair && (r.certain < 0 || r.certain >= V);
-                if (lane == 0) p.d_tv[(int64_t)b * k + j] = bad || nowhere ? 1.f : (float)(0.5 * (total + under));
-                if (bad) flags |= METASD_STATUS_NONFINITE;
+            double w[PER], mine = 0.0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                w[i] = 0.0;
+                if (i < per && lane * per + i < parts) w[i] = sh_weight[lane * per + i];
             }
-            if (draws) {
-                int token = -1;
-                if (bad) {
-                    flags |= METASD_STATUS_NONFINITE;
-                } else if (total > 0.0) {
-                    const double threshold = (double)__ldg(p.u_draw + b) * total;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) mine += w[i];
+            const double upto = lanes_up_to(mine), total = __shfl_sync(FULL, upto, 31);
+            const bool bad = !(total < INFINITY);
+            if (bad) flags |= METASD_STATUS_NONFINITE;
+            Crossing x = {0.0, 0.0, 0, 0, -1, false};      // nothing to look for
+            if (n == j) {       // the row that the token is drawn from
+                if (total > 0.0 && !bad) {
+                    x.threshold = (double)u_draw * total;
+                    if (x.threshold < 0.0) x.threshold = 0.0;
                     bool beyond;
-                    const int src = crossing_lane(mine, upto, threshold, beyond);
-                    int part = -1;
-                    double base = 0.0;
-                    if (lane == src) {
-                        double run = upto - mine;
-                        bool done = false;
-                        for (int i = 0; i < per; ++i) {
-                            const double w = lane * per + i < parts ? sh_weight[lane * per + i] : 0.0;
-                            if (!done && w > 0.0) {
-                                part = lane * per + i;
-                                base = run;
-                                done = run + w > threshold;
-                            }
-                            run += w;
+                    const int src = crossing_lane(mine, upto, x.threshold, beyond);
+                    int part = -1;      // of the lane's: the first that ends beyond the threshold, else the last with weight
+                    double run = upto - mine;
+                    bool done = false;
+#pragma unroll
+                    for (int i = 0; i < PER; ++i) {
+                        if (!done && w[i] > 0.0) {
+                            part = lane * per + i;
+                            x.base = run;
                         }
+                        run += w[i];
+                        done = done || (w[i] > 0.0 && run > x.threshold);
                     }
                     part = __shfl_sync(FULL, part, src);
-                    base = __shfl_sync(FULL, base, src);
-                    token = find_token<LT>(r, pair, part * part_vecs, min((part + 1) * part_vecs, r.n_vec), base, threshold);
-                } else if (pair || r.certain >= 0) {
-                    again = true;       // nothing is left over of the target's row: it is drawn from as it stands
+                    x.base = fmin(__shfl_sync(FULL, x.base, src), x.threshold);
+                    x.g0 = part * part_vecs;
+                    x.g1 = min(x.g0 + part_vecs, r.n_vec);
+                } else if (!bad && (pair || r.certain >= 0)) {
+                    x.again = true;
                 } else {
-                    flags |= METASD_STATUS_NONFINITE;       // a row of zeros
-                }
-                if (!again && lane == 0) {
-                    p.accepted_len[b] = n;
-                    p.next_token[b] = token;
+                    flags |= METASD_STATUS_NONFINITE;       // or a row of zeros
                 }
             }
-            if (!again && flags && lane == 0 && p.status) atomicOr(p.status, flags);
-            if (lane == 0) sh_again = again;
+            if (lane == 0) sh_crossing = x;
+            if (TV && first && j < kb) {
+                double apart = 0.0;
+#pragma unroll
+                for (int i = 0; i < PER; ++i)
+                    if (i < per && lane * per + i < parts) apart += (double)sh_apart[lane * per + i];
+                apart = warp_sum(apart);
+                // a token outside the vocabulary has no place in the row
+                const bool nowhere = !pair && (r.certain < 0 || r.certain >= V);
+                if (lane == 0) p.d_tv[(int64_t)b * k + j] = bad || nowhere ? 1.f : (float)(0.5 * apart);
+            }
+            if (lane == 0) {
+                if (n == j && !x.again) p.accepted_len[b] = n;
+                if (flags && !x.again && p.status) atomicOr(p.status, flags);
+            }
         }
         __syncthreads();
-        if (!sh_again) return;
+        if (!sh_crossing.again) break;
+        __syncthreads();
         r.certain = -1;
         pair = false;
-        for (int s = warp; s < parts; s += PROBS_WARPS) {
-            const Sums x = sum_part<LT, false>(r, false, s * part_vecs, min((s + 1) * part_vecs, r.n_vec));
-            const double w = warp_sum(weight_of(x));
-            if (lane == 0) sh_weight[s] = w;
-        }
+        sum_parts<LT, true, TV>(r, false, part_vecs, warp, parts, WARPS, smem_addr(sh_weight), smem_addr(sh_apart));
         __syncthreads();
     }
+    if (TV && n != j) return;
+    const int token = find_token<LT>(r, pair, sh_crossing, sh_warp);
+    if (token >= 0 || (tid == 0 && sh_crossing.g0 == sh_crossing.g1)) p.next_token[b] = token;
 }
 
 // The reward of a round that metasd_verify did not verify, the bandit update and the next selection: a warp per sequence.
@@ -498,14 +587,14 @@ cudaError_t launch_probs(const ProbsParams &params, int dtype, int n_sm, cudaStr
     p.part_vecs = (int)(step * std::max(1ll, (n_vec + step * MAX_PARTS - 1) / (step * MAX_PARTS)));
     p.parts = (int)((n_vec + p.part_vecs - 1) / p.part_vecs);
     const long long jobs = (long long)p.batch * (p.d_tv ? p.k + 1 : 1);
+    // rows that are read: with distances the bonus row of a few sequences only, and of ragged drafts about half
+    const long long rows = p.d_tv ? (long long)p.batch * (p.draft_len ? (p.k + 1) / 2 : p.k) : p.batch;
+    // As many blocks of a cluster as leave all rows in flight at once (four blocks fit an SM) and every warp a part.
     int cluster = 1;
-    while (cluster < 8 && jobs * cluster < 2 * n_sm && p.parts > PROBS_WARPS * cluster) cluster *= 2;
-    const unsigned grid = (unsigned)(jobs * cluster);
-    if (dtype == METASD_BF16)
-        return p.d_tv ? launch_kernel(probs_kernel<__nv_bfloat16, true>, grid, PROBS_THREADS, 0, cluster, true, stream, p)
-                      : launch_kernel(probs_kernel<__nv_bfloat16, false>, grid, PROBS_THREADS, 0, cluster, true, stream, p);
-    return p.d_tv ? launch_kernel(probs_kernel<float, true>, grid, PROBS_THREADS, 0, cluster, true, stream, p)
-                  : launch_kernel(probs_kernel<float, false>, grid, PROBS_THREADS, 0, cluster, true, stream, p);
+    while (cluster < 8 && 2 * rows * cluster <= 4 * n_sm && p.parts > WARPS * cluster) cluster *= 2;
+    auto launch = [&](auto kernel) { return launch_kernel(kernel, (unsigned)(jobs * cluster), THREADS, 0, cluster, true, stream, p); };
+    if (dtype == METASD_BF16) return p.d_tv ? launch(probs_kernel<__nv_bfloat16, true>) : launch(probs_kernel<__nv_bfloat16, false>);
+    return p.d_tv ? launch(probs_kernel<float, true>) : launch(probs_kernel<float, false>);
 }
 
 cudaError_t launch_feedback(const VerifyParams &p, const float *d_tv, cudaStream_t stream)
