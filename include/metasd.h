@@ -104,7 +104,8 @@ enum metasd_path {
                                          not planned (their slots are -1) */
 #define METASD_STATUS_TRUNCATED 256u  /* metasd_cache_plan: the step has more than max_tokens entries; the sequences that did not fit
                                          are not planned */
-#define METASD_STATUS_BAD_STATE 512u  /* a cache's counts are outside their range, or more blocks came back than it has */
+#define METASD_STATUS_BAD_STATE 512u  /* a cache's counts are outside their range (they are taken as the nearest in it), or more blocks
+                                         would come back to a pool than its list has room for: none does */
 #define METASD_STATUS_BAD_POINTER 16u /* the drafter table of a call held a NULL or misaligned entry: its rows are never
                                         read and the outputs of the sequences that played that drafter are meaningless */
 
@@ -343,7 +344,8 @@ typedef struct metasd_cache {
     int32_t *held;          /* [n_pools, max_batch] */
     int32_t *free_blocks;   /* [n_pools, n_blocks]: a stack of the pool's free blocks; the first free_count count */
     int32_t *free_count;    /* [n_pools] */
-    void *workspace;        /* metasd_cache_workspace_bytes(max_batch, n_pools) bytes, 16-byte aligned, of this cache alone */
+    void *workspace;        /* metasd_cache_workspace_bytes(max_batch, n_pools) bytes, 16-byte aligned, of this cache alone; nothing in
+                               it is kept between calls */
     uint32_t *status;       /* optional: METASD_STATUS_* bits are OR-ed into it */
     int32_t n_pools;        /* 1 .. METASD_MAX_POOLS */
     int32_t max_batch;      /* 1 .. 65535 */

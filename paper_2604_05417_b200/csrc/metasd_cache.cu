@@ -18,24 +18,18 @@ namespace metasd {
 
 namespace {
 
-constexpr int PLAN_THREADS = 1024, PLAN_WARPS = PLAN_THREADS / 32;
+constexpr int MOST_THREADS = 1024, MOST_WARPS = 32;
 constexpr int KEYS = METASD_MAX_POOLS + 1;      // the pools, and who takes no part
-constexpr int FILL_THREADS = 256;
-constexpr int SPAN = 2048;                      // entries that a block deals with at once
-constexpr int RELEASE_THREADS = 1024, RELEASE_WARPS = RELEASE_THREADS / 32;
+constexpr int FILL_THREADS = 256, SPAN = 2048;  // of the second kernel: entries that a block deals with at once
+constexpr int STARTS = 2048;                    // places whose first entries a block keeps in shared memory
 constexpr unsigned FULL = 0xFFFFFFFFu;
 
 // What the plan knows of the sequence at a place (workspace).  `first` is its position in the free list of the first block it
 // takes (the next ones lie in front of it) or -1: it is not served.
 struct __align__(16) PlanEntry {
     int32_t sequence, pool, cached, held;
-    int32_t fresh, need, first, unused;
+    int32_t fresh, need, first, leads;      // leads: the pool's first place
 };
-// A sequence's part of a release (workspace): `drop` blocks from `from` on go to `to`, `to - 1`, .. of the pool's free list.
-struct __align__(16) ReleaseEntry {
-    int32_t from, drop, to, unused;
-};
-
 template <typename T> __device__ __forceinline__ T warp_sum_up_to(T x)
 {
     const int lane = threadIdx.x & 31;
@@ -43,6 +37,18 @@ template <typename T> __device__ __forceinline__ T warp_sum_up_to(T x)
     for (int o = 1; o < 32; o <<= 1) {
         const T t = __shfl_up_sync(FULL, x, o);
         if (lane >= o) x += t;
+    }
+    return x;
+}
+// Running sums that stop at 2^31 - 1: entries behind that have no place in any output.
+__device__ __forceinline__ uint32_t add_up(uint32_t a, uint32_t b) { return min(a + b, 0x7FFFFFFFu); }
+__device__ __forceinline__ uint32_t warp_add_up_to(uint32_t x)
+{
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t t = __shfl_up_sync(FULL, x, o);
+        if (lane >= o) x = add_up(x, t);
     }
     return x;
 }
@@ -62,54 +68,15 @@ __device__ __forceinline__ int pool_of(const CachePlanParams &p, int b, uint32_t
     return g < 0 || g >= p.c.n_pools ? p.c.n_pools : g;
 }
 
-// The places of a span's entries, by one block: sh_at[i] = place of entry `begin + i`.
-template <int THREADS>
-__device__ __forceinline__ void places_of_span(const int32_t *token_start, int batch, int begin, int end, int *sh_at, int *sh_warp)
+// The last place from lo on (token_start[lo] <= t) and in front of hi that starts at or in front of entry t: entry t is its.
+__device__ __forceinline__ int place_of(const int32_t *token_start, int lo, int hi, int t)
 {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    constexpr int PER = SPAN / THREADS;
-    // the last place that starts at or in front of `begin` (every warp looks for itself): 32 probes a step
-    int lo = 0, hi = batch;     // token_start[lo] <= begin, and < token_start[hi] or hi == batch
     while (hi - lo > 1) {
-        const int step = (hi - lo + 31) / 32;
-        const int at = min(lo + lane * step, hi);
-        const unsigned below = __ballot_sync(FULL, at < hi && __ldcg(token_start + at) <= begin);
-        const int last = 31 - __clz(below);     // lane 0 always is
-        hi = min(lo + (last + 1) * step, hi);
-        lo = lo + last * step;
+        const int mid = (lo + hi) >> 1;
+        if (token_start[mid] <= t) lo = mid;
+        else hi = mid;
     }
-    for (int i = tid; i < SPAN; i += THREADS) sh_at[i] = 0;
-    __syncthreads();
-    if (tid == 0) sh_at[0] = lo;
-    __syncthreads();
-    // every place that starts inside the span marks its first entry; the largest of those that start together has entries
-    for (int at = lo + 1 + tid; at < batch; at += THREADS) {
-        const int start = __ldcg(token_start + at);
-        if (start >= end) break;
-        atomicMax(sh_at + (start - begin), at);
-    }
-    __syncthreads();
-    // running maximum
-    int mine[PER], top = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        top = max(top, sh_at[tid * PER + i]);
-        mine[i] = top;
-    }
-    int upto = top;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int t = __shfl_up_sync(FULL, upto, o);
-        if (lane >= o) upto = max(upto, t);
-    }
-    if (lane == 31) sh_warp[warp] = upto;
-    int before = __shfl_up_sync(FULL, upto, 1);
-    if (lane == 0) before = 0;
-    __syncthreads();
-    for (int w = 0; w < warp; ++w) before = max(before, sh_warp[w]);
-#pragma unroll
-    for (int i = 0; i < PER; ++i) sh_at[tid * PER + i] = max(mine[i], before);
-    __syncthreads();
+    return lo;
 }
 
 // Entry t: its slot, position and sequence.  The first entry of a block that is taken writes the block table.
@@ -140,303 +107,424 @@ __device__ __forceinline__ Entry entry_at(const CachePlanParams &p, const PlanEn
     return r;
 }
 
+// Entries begin .. end - 1, by one block, two to a thread.
 template <int THREADS>
-__device__ __forceinline__ void fill_span(const CachePlanParams &p, int begin, int end, int *sh_at, int *sh_warp)
+__device__ __forceinline__ void fill(const CachePlanParams &p, const PlanEntry *entries, const int32_t *token_start, int begin, int end)
 {
-    const PlanEntry *entries = (const PlanEntry *)p.c.workspace;
-    places_of_span<THREADS>(p.token_start, p.batch, begin, end, sh_at, sh_warp);
-    for (int i = 2 * threadIdx.x; begin + i < end; i += 2 * THREADS) {
-        const int t = begin + i;
-        const Entry a = entry_at(p, entries, p.token_start, sh_at[i], t);
-        if (t + 1 < end && p.wide) {
-            const Entry b = entry_at(p, entries, p.token_start, sh_at[i + 1], t + 1);
-            *reinterpret_cast<longlong2 *>(p.slot_map + t) = make_longlong2(a.slot, b.slot);
-            if (p.position) *reinterpret_cast<int2 *>(p.position + t) = make_int2(a.position, b.position);
-            if (p.sequence) *reinterpret_cast<int2 *>(p.sequence + t) = make_int2(a.sequence, b.sequence);
-        } else {
-            p.slot_map[t] = a.slot;
-            if (p.position) p.position[t] = a.position;
-            if (p.sequence) p.sequence[t] = a.sequence;
-            if (t + 1 < end) {
-                const Entry b = entry_at(p, entries, p.token_start, sh_at[i + 1], t + 1);
-                p.slot_map[t + 1] = b.slot;
-                if (p.position) p.position[t + 1] = b.position;
-                if (p.sequence) p.sequence[t + 1] = b.sequence;
+    const int lo = place_of(token_start, 0, p.batch, begin), hi = place_of(token_start, lo, p.batch, end - 1) + 1;
+    for (int t = begin + 2 * (int)threadIdx.x; t < end; t += 2 * THREADS) {
+        const int at = place_of(token_start, lo, hi, t);
+        const Entry a = entry_at(p, entries, token_start, at, t);
+        if (t + 1 < end) {
+            const int next = token_start[at + 1] > t + 1 ? at : place_of(token_start, at + 1, hi, t + 1);
+            const Entry b = entry_at(p, entries, token_start, next, t + 1);
+            if (p.wide) {
+                *reinterpret_cast<longlong2 *>(p.slot_map + t) = make_longlong2(a.slot, b.slot);
+                if (p.position) *reinterpret_cast<int2 *>(p.position + t) = make_int2(a.position, b.position);
+                if (p.sequence) *reinterpret_cast<int2 *>(p.sequence + t) = make_int2(a.sequence, b.sequence);
+                continue;
+            }
+            p.slot_map[t + 1] = b.slot;
+            if (p.position) p.position[t + 1] = b.position;
+            if (p.sequence) p.sequence[t + 1] = b.sequence;
+        }
+        p.slot_map[t] = a.slot;
+        if (p.position) p.position[t] = a.position;
+        if (p.sequence) p.sequence[t] = a.sequence;
+    }
+}
+
+// Shared memory of the first kernel.
+template <int THREADS> struct PlanShared {
+    int tally[KEYS][MOST_WARPS];        // sequences of a pool in front of a warp's, then the places behind them
+    int total[KEYS];
+    int start[KEYS + 1];
+    long long need[MOST_WARPS];
+    uint32_t tokens[MOST_WARPS];
+    long long base[KEYS];               // running sum of the blocks at a pool's first place
+    int free[KEYS], taken[KEYS];
+    int token_start[STARTS + 1];
+    PlanEntry entries[THREADS];         // by place, where a thread has one sequence
+};
+
+// The sequence's entry of the plan, as far as it is known without the others.
+__device__ __forceinline__ PlanEntry plan_entry(const CachePlanParams &p, int b, int g, uint32_t &flags)
+{
+    const metasd_cache &c = p.c;
+    PlanEntry e = {b, g, 0, 0, 0, 0, -1, 0};
+    if (g >= c.n_pools) return e;
+    const int cached = __ldg(p.cached + g * p.cached_pool + b), length = __ldg(p.length + b), held = c.held[(int64_t)g * c.max_batch + b];
+    const int kept = min(max(held, 0), c.max_blocks);
+    if (kept != held) flags |= METASD_STATUS_BAD_STATE;
+    // a cache that the table does not cover, or a length that it cannot: nothing is planned
+    const bool bad = cached < 0 || length < 0 || (int64_t)cached > (int64_t)kept * c.page_size || (int64_t)length > (int64_t)c.max_blocks * c.page_size;
+    if (bad) {
+        flags |= METASD_STATUS_BAD_LENGTH;
+        return e;
+    }
+    e.cached = cached;
+    e.held = kept;
+    e.fresh = max(length - cached, 0);
+    if (e.fresh) e.need = max(divide(length - 1, c.page_size, p.page_inverse) + 1 - kept, 0);
+    return e;
+}
+
+// What the sums say about the place: whether it is planned, and from where in the free list it takes its blocks.
+template <int THREADS>
+__device__ __forceinline__ void serve(const CachePlanParams &p, PlanShared<THREADS> &sh, PlanEntry &e, int at, uint32_t start, long long before, uint32_t &flags)
+{
+    const metasd_cache &c = p.c;
+    const uint32_t end = add_up(start, (uint32_t)e.fresh);
+    p.token_start[at] = (int32_t)start;
+    if (at == p.batch - 1) p.token_start[p.batch] = (int32_t)end;
+    if (at <= STARTS) sh.token_start[at] = (int32_t)start;
+    if (at == p.batch - 1 && at < STARTS) sh.token_start[p.batch] = (int32_t)end;
+    if (e.fresh) {
+        const bool room = (long long)start + e.fresh <= p.max_tokens, enough = e.need == 0 || before + e.need <= sh.free[e.pool];
+        if (!room) flags |= METASD_STATUS_TRUNCATED;
+        if (!enough) flags |= METASD_STATUS_NO_BLOCKS;
+        if (room && enough) {
+            e.first = e.need ? sh.free[e.pool] - 1 - (int)before : 0;
+            if (e.need) {
+                atomicMax(sh.taken + e.pool, (int)(before + e.need));
+                c.held[(int64_t)e.pool * c.max_batch + e.sequence] = e.held + e.need;
             }
         }
     }
 }
 
-template <bool ALONE> __global__ void __launch_bounds__(PLAN_THREADS) plan_kernel(const CachePlanParams p)
+// The free lists' lengths, and none taken yet.
+template <int THREADS> __device__ __forceinline__ void look_at_pools(const CachePlanParams &p, PlanShared<THREADS> &sh, uint32_t &flags)
 {
-    __shared__ int sh_tally[KEYS][PLAN_WARPS];      // sequences of a pool in front of a warp's, then the places behind them
-    __shared__ int sh_start[KEYS + 1];
-    __shared__ long long sh_tokens[PLAN_WARPS], sh_need[PLAN_WARPS];
-    __shared__ long long sh_base[KEYS];             // running sum of the blocks at a pool's first place
-    __shared__ int sh_free[KEYS], sh_taken[KEYS];
-    __shared__ int sh_at[ALONE ? SPAN : 1], sh_warp[PLAN_WARPS];
-    __shared__ int sh_total;
+    for (int i = threadIdx.x; i < p.c.n_pools; i += THREADS) {
+        const int free = p.c.free_count[i];
+        sh.free[i] = min(max(free, 0), p.c.n_blocks);
+        sh.taken[i] = 0;
+        if (sh.free[i] != free) flags |= METASD_STATUS_BAD_STATE;
+    }
+}
 
-    launch_dependents();
-    grid_dependency_wait();
-    const metasd_cache &c = p.c;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, batch = p.batch, P = c.n_pools;
-    PlanEntry *entries = (PlanEntry *)c.workspace;
+// Order, running sums and the block tables' growth of a step, by one block with a sequence (then a place) per thread, in registers
+// and shared memory.
+template <int THREADS> __device__ __forceinline__ void plan_step(const CachePlanParams &p, PlanShared<THREADS> &sh)
+{
+    constexpr int WARPS = THREADS / 32;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, batch = p.batch, P = p.c.n_pools;
+    const bool in = tid < batch;
     uint32_t flags = 0;
-    for (int i = tid; i < KEYS * PLAN_WARPS; i += PLAN_THREADS) (&sh_tally[0][0])[i] = 0;
-    for (int i = tid; i < P; i += PLAN_THREADS) {
-        sh_free[i] = min(max(c.free_count[i], 0), c.n_blocks);
-        sh_taken[i] = 0;
-        if (sh_free[i] != c.free_count[i]) flags |= METASD_STATUS_BAD_STATE;
+    PlanEntry e = {tid, P, 0, 0, 0, 0, -1, 0};
+    if (in) e = plan_entry(p, tid, pool_of(p, tid, flags), flags);
+    look_at_pools<THREADS>(p, sh, flags);
+    if (p.pool) {       // order by pool: a counting sort
+        for (int g = lane; g <= P; g += 32) sh.tally[g][warp] = 0;
+        __syncwarp();
+        const unsigned same = __match_any_sync(FULL, in ? e.pool : -1);
+        const int rank = __popc(same & ((1u << lane) - 1u));
+        if (in && rank == 0) sh.tally[e.pool][warp] = __popc(same);
+        __syncthreads();
+        for (int g = warp; g <= P; g += WARPS) {
+            const int x = lane < WARPS ? sh.tally[g][lane] : 0, upto = warp_sum_up_to(x);
+            if (lane < WARPS) sh.tally[g][lane] = upto - x;
+            if (lane == 31) sh.total[g] = upto;
+        }
+        __syncthreads();
+        const int x = lane < P ? sh.total[lane] : 0, upto = warp_sum_up_to(x);
+        const int start = __shfl_sync(FULL, upto - x, e.pool & 31), behind = __shfl_sync(FULL, upto, 31);
+        if (in) {
+            const int at = (e.pool < P ? start : behind) + sh.tally[e.pool][warp] + rank;
+            e.leads = e.pool < P && at == start;
+            sh.entries[at] = e;
+            if (p.order) p.order[at] = tid;
+            if (p.place) p.place[tid] = at;
+        }
+        if (p.pool_start && warp == 0) {
+            if (lane < P) p.pool_start[lane] = upto - x;
+            if (lane == 0) p.pool_start[P] = behind;
+        }
+        __syncthreads();
+        if (in) e = sh.entries[tid];
+    } else {
+        if (in && p.order) p.order[tid] = tid;
+        if (in && p.place) p.place[tid] = tid;
+        if (p.pool_start && tid <= P) p.pool_start[tid] = tid == 0 ? 0 : batch;
     }
+    // running sums of the entries and of the blocks
+    const uint32_t tokens = in ? (uint32_t)e.fresh : 0u, upto_tokens = warp_add_up_to(tokens);
+    const long long need = in ? e.need : 0, upto_need = warp_sum_up_to(need);
+    if (lane == 31) { sh.tokens[warp] = upto_tokens; sh.need[warp] = upto_need; }
     __syncthreads();
+    const uint32_t tokens_w = warp_add_up_to(lane < WARPS ? sh.tokens[lane] : 0u);
+    const long long need_w = warp_sum_up_to(lane < WARPS ? sh.need[lane] : 0ll);
+    uint32_t tokens0 = __shfl_sync(FULL, tokens_w, (warp + 31) & 31), before_lane = __shfl_up_sync(FULL, upto_tokens, 1);
+    long long need0 = __shfl_sync(FULL, need_w, (warp + 31) & 31);
+    if (warp == 0) { tokens0 = 0u; need0 = 0; }
+    if (lane == 0) before_lane = 0u;
+    const long long blocks = need0 + upto_need - need;
+    if (p.pool) {
+        if (in && e.leads) sh.base[e.pool] = blocks;
+        __syncthreads();
+    }
+    if (in) {
+        serve(p, sh, e, tid, add_up(tokens0, before_lane), p.pool && e.fresh ? blocks - sh.base[e.pool] : blocks, flags);
+        sh.entries[tid] = e;
+        ((PlanEntry *)p.c.workspace)[tid] = e;
+    }
+    flags = __reduce_or_sync(FULL, flags);
+    if (flags && lane == 0 && p.c.status) atomicOr(p.c.status, flags);
+    __syncthreads();
+    for (int i = tid; i < P; i += THREADS) p.c.free_count[i] = sh.free[i] - sh.taken[i];
+}
 
-    // ---- order by pool: a warp takes rows of 32 sequences, one behind the other
-    const int rows = (batch + 31) / 32, row0 = (int)((long long)rows * warp / PLAN_WARPS), row1 = (int)((long long)rows * (warp + 1) / PLAN_WARPS);
+// The same for more sequences than a block has threads: a warp takes rows of 32, one behind the other, through the workspace.
+__device__ __forceinline__ void plan_rows(const CachePlanParams &p, PlanShared<MOST_THREADS> &sh)
+{
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, batch = p.batch, P = p.c.n_pools;
+    PlanEntry *entries = (PlanEntry *)p.c.workspace;
+    uint32_t flags = 0;
+    for (int i = tid; i < (P + 1) * MOST_WARPS; i += MOST_THREADS) (&sh.tally[0][0])[i] = 0;
+    look_at_pools<MOST_THREADS>(p, sh, flags);
+    __syncthreads();
+    const int rows = (batch + 31) / 32, row0 = rows * warp / MOST_WARPS, row1 = rows * (warp + 1) / MOST_WARPS;
     for (int row = row0; row < row1; ++row) {
-        const int b = row * 32 + lane;
-        const unsigned here = __ballot_sync(FULL, b < batch);
-        if (b < batch) {
-            const int g = pool_of(p, b, flags);
-            const unsigned same = __match_any_sync(here, g);
-            if (lane == __ffs(same) - 1) sh_tally[g][warp] += __popc(same);
-        }
+        const int b = row * 32 + lane, g = b < batch ? pool_of(p, b, flags) : -1;
+        const unsigned same = __match_any_sync(FULL, g);
+        if (b < batch && lane == __ffs(same) - 1) sh.tally[g][warp] += __popc(same);
         __syncwarp();
     }
     __syncthreads();
-    for (int g = warp; g <= P; g += PLAN_WARPS) {
-        const int x = sh_tally[g][lane], upto = warp_sum_up_to(x);
-        sh_tally[g][lane] = upto - x;
-        if (lane == 31) sh_start[g + 1] = upto;
+    for (int g = warp; g <= P; g += MOST_WARPS) {
+        const int x = sh.tally[g][lane], upto = warp_sum_up_to(x);
+        sh.tally[g][lane] = upto - x;
+        if (lane == 31) sh.total[g] = upto;
     }
     __syncthreads();
-    if (tid == 0) {
-        sh_start[0] = 0;
-        for (int g = 0; g <= P; ++g) sh_start[g + 1] += sh_start[g];
-        if (p.pool_start)
-            for (int g = 0; g <= P; ++g) p.pool_start[g] = sh_start[g];
+    if (warp == 0) {
+        const int x = lane < P ? sh.total[lane] : 0, upto = warp_sum_up_to(x);
+        if (lane < P) sh.start[lane] = upto - x;
+        if (lane == 31) sh.start[P] = upto;
+        if (p.pool_start && lane < P) p.pool_start[lane] = upto - x;
+        if (p.pool_start && lane == 31) p.pool_start[P] = upto;
     }
     __syncthreads();
     for (int row = row0; row < row1; ++row) {
         const int b = row * 32 + lane;
-        const unsigned here = __ballot_sync(FULL, b < batch);
-        int g = 0, at = 0;
-        unsigned same = 0;
-        if (b < batch) {
-            uint32_t seen = 0;
-            g = pool_of(p, b, seen);
-            same = __match_any_sync(here, g);
-            at = sh_start[g] + sh_tally[g][warp] + __popc(same & ((1u << lane) - 1u));
-        }
+        uint32_t seen = 0;
+        const int g = b < batch ? pool_of(p, b, seen) : -1;
+        const unsigned same = __match_any_sync(FULL, g);
+        int at = 0;
+        if (b < batch) at = sh.start[g] + sh.tally[g][warp] + __popc(same & ((1u << lane) - 1u));
         __syncwarp();
         if (b < batch) {
-            if (lane == __ffs(same) - 1) sh_tally[g][warp] += __popc(same);
-            PlanEntry e = {b, g, 0, 0, 0, 0, -1, 0};
-            if (g < P) {
-                const int64_t row_of = (int64_t)g * c.max_batch + b;
-                const int cached = __ldg(p.cached + g * p.cached_pool + b), length = __ldg(p.length + b), held = c.held[row_of];
-                const int kept = min(max(held, 0), c.max_blocks);
-                if (kept != held) flags |= METASD_STATUS_BAD_STATE;
-                // a cache that the table does not cover, or a length that it cannot: nothing is planned
-                const bool bad = cached < 0 || length < 0 || (int64_t)cached > (int64_t)kept * c.page_size || (int64_t)length > (int64_t)c.max_blocks * c.page_size;
-                if (bad) {
-                    flags |= METASD_STATUS_BAD_LENGTH;
-                } else {
-                    e.cached = cached;
-                    e.held = kept;
-                    e.fresh = max(length - cached, 0);
-                    if (e.fresh) e.need = max(divide(length - 1, c.page_size, p.page_inverse) + 1 - kept, 0);
-                }
-            }
-            entries[at] = e;
+            if (lane == __ffs(same) - 1) sh.tally[g][warp] += __popc(same);
+            entries[at] = plan_entry(p, b, g, flags);
             if (p.order) p.order[at] = b;
             if (p.place) p.place[b] = at;
         }
         __syncwarp();
     }
     __syncthreads();
-
-    // ---- running sums of the entries and of the blocks, in that order
-    long long tokens = 0, need = 0;
+    uint32_t tokens = 0;
+    long long need = 0;
     for (int row = row0; row < row1; ++row) {
         const int at = row * 32 + lane;
         if (at < batch) {
-            tokens += entries[at].fresh;
+            tokens = add_up(tokens, (uint32_t)entries[at].fresh);
             need += entries[at].need;
         }
     }
-    tokens = warp_total(tokens);
-    need = warp_total(need);
-    if (lane == 0) { sh_tokens[warp] = tokens; sh_need[warp] = need; }
+    tokens = warp_add_up_to(tokens);
+    need = warp_sum_up_to(need);
+    if (lane == 31) { sh.tokens[warp] = tokens; sh.need[warp] = need; }
     __syncthreads();
-    {
-        const long long t = sh_tokens[lane], n = sh_need[lane];
-        const long long before_t = warp_sum_up_to(t) - t, before_n = warp_sum_up_to(n) - n;
-        tokens = __shfl_sync(FULL, before_t, warp);
-        need = __shfl_sync(FULL, before_n, warp);
-    }
-    const long long tokens0 = tokens, need0 = need;
+    const uint32_t tokens_w = warp_add_up_to(sh.tokens[lane]);
+    const long long need_w = warp_sum_up_to(sh.need[lane]);
+    tokens = __shfl_sync(FULL, tokens_w, (warp + 31) & 31);
+    need = __shfl_sync(FULL, need_w, (warp + 31) & 31);
+    if (warp == 0) { tokens = 0u; need = 0; }
+    long long run = need;
     for (int row = row0; row < row1; ++row) {
         const int at = row * 32 + lane;
         const int n = at < batch ? entries[at].need : 0;
         const long long upto = warp_sum_up_to((long long)n);
         if (at < batch) {
             const int g = entries[at].pool;
-            if (g < P && at == sh_start[g]) sh_base[g] = need + upto - n;
+            if (g < P && at == sh.start[g]) sh.base[g] = run + upto - n;
         }
-        need += __shfl_sync(FULL, upto, 31);
+        run += __shfl_sync(FULL, upto, 31);
     }
     __syncthreads();
-    need = need0;
-    tokens = tokens0;
     for (int row = row0; row < row1; ++row) {
         const int at = row * 32 + lane;
-        const int fresh = at < batch ? entries[at].fresh : 0, n = at < batch ? entries[at].need : 0;
-        const long long upto_t = warp_sum_up_to((long long)fresh), upto_n = warp_sum_up_to((long long)n);
+        PlanEntry e = {0, P, 0, 0, 0, 0, -1, 0};
+        if (at < batch) e = entries[at];
+        const uint32_t upto_t = warp_add_up_to((uint32_t)e.fresh);
+        const long long upto_n = warp_sum_up_to((long long)e.need);
+        uint32_t before_lane = __shfl_up_sync(FULL, upto_t, 1);
+        if (lane == 0) before_lane = 0u;
         if (at < batch) {
-            const int g = entries[at].pool;
-            const long long start = tokens + upto_t - fresh;
-            p.token_start[at] = (int32_t)min(start, 0x7FFFFFFFll);
-            if (at == batch - 1) p.token_start[batch] = sh_total = (int32_t)min(start + fresh, 0x7FFFFFFFll);
-            if (fresh) {
-                const long long before = need + upto_n - n - sh_base[g];
-                const bool room = start + fresh <= p.max_tokens, enough = n == 0 || before + n <= sh_free[g];
-                if (!room) flags |= METASD_STATUS_TRUNCATED;
-                if (!enough) flags |= METASD_STATUS_NO_BLOCKS;
-                if (room && enough) {
-                    entries[at].first = n ? sh_free[g] - 1 - (int)before : 0;
-                    if (n) {
-                        atomicMax(sh_taken + g, (int)(before + n));
-                        c.held[(int64_t)g * c.max_batch + entries[at].sequence] = entries[at].held + n;
-                    }
-                }
-            }
+            serve(p, sh, e, at, add_up(tokens, before_lane), e.fresh ? need + upto_n - e.need - sh.base[e.pool] : 0, flags);
+            entries[at].first = e.first;
         }
-        tokens += __shfl_sync(FULL, upto_t, 31);
+        tokens = add_up(tokens, __shfl_sync(FULL, upto_t, 31));
         need += __shfl_sync(FULL, upto_n, 31);
     }
     flags = __reduce_or_sync(FULL, flags);
-    if (flags && lane == 0 && c.status) atomicOr(c.status, flags);
+    if (flags && lane == 0 && p.c.status) atomicOr(p.c.status, flags);
     __syncthreads();
-    for (int i = tid; i < P; i += PLAN_THREADS) c.free_count[i] = sh_free[i] - sh_taken[i];
-    if constexpr (ALONE) {
-        const int total = min(sh_total, p.max_tokens);
-        for (int begin = 0; begin < total; begin += SPAN) {
-            fill_span<PLAN_THREADS>(p, begin, min(begin + SPAN, total), sh_at, sh_warp);
-            __syncthreads();
+    for (int i = tid; i < P; i += MOST_THREADS) p.c.free_count[i] = sh.free[i] - sh.taken[i];
+}
+
+// FILLS: a cluster; its first block plans, then all of them write the entries.
+template <int THREADS, bool FILLS> __global__ void __launch_bounds__(THREADS) plan_kernel(const CachePlanParams p)
+{
+    __shared__ PlanShared<THREADS> sh;
+    launch_dependents();
+    grid_dependency_wait();
+    const int rank = FILLS ? (int)cluster_rank() : 0, batch = p.batch;
+    if (rank == 0) {
+        if constexpr (THREADS == MOST_THREADS) {
+            if (batch <= THREADS) plan_step<THREADS>(p, sh);
+            else plan_rows(p, sh);
+        } else {
+            plan_step<THREADS>(p, sh);
         }
+    }
+    if constexpr (FILLS) {
+        const int ranks = (int)cluster_size();
+        if (ranks > 1) cluster_sync_all();
+        const int32_t *token_start = p.token_start;
+        const PlanEntry *entries = (const PlanEntry *)p.c.workspace;
+        if (batch <= STARTS) {
+            if (rank != 0) {
+                for (int i = threadIdx.x; i <= batch; i += THREADS) sh.token_start[i] = __ldcg(p.token_start + i);
+                __syncthreads();
+            }
+            token_start = sh.token_start;
+        }
+        if (rank == 0 && batch <= THREADS) entries = sh.entries;
+        const int total = min(token_start[batch], p.max_tokens), share = 2 * THREADS;
+        for (long long begin = (long long)share * rank; begin < total; begin += (long long)share * ranks)
+            fill<THREADS>(p, entries, token_start, (int)begin, (int)min(begin + share, (long long)total));
     }
 }
 
 __global__ void __launch_bounds__(FILL_THREADS) fill_kernel(const CachePlanParams p)
 {
-    __shared__ int sh_at[SPAN], sh_warp[FILL_THREADS / 32];
+    __shared__ int32_t sh_start[STARTS + 1];
     launch_dependents();
     grid_dependency_wait();
-    const int total = min(p.token_start[p.batch], p.max_tokens);
-    for (long long begin = (long long)blockIdx.x * SPAN; begin < total; begin += (long long)gridDim.x * SPAN) {
-        fill_span<FILL_THREADS>(p, (int)begin, (int)min(begin + SPAN, (long long)total), sh_at, sh_warp);
+    const int32_t *token_start = p.token_start;
+    if (p.batch <= STARTS) {
+        for (int i = threadIdx.x; i <= p.batch; i += FILL_THREADS) sh_start[i] = __ldcg(p.token_start + i);
         __syncthreads();
+        token_start = sh_start;
     }
+    const int total = min(token_start[p.batch], p.max_tokens);
+    for (long long begin = (long long)blockIdx.x * SPAN; begin < total; begin += (long long)gridDim.x * SPAN)
+        fill<FILL_THREADS>(p, (const PlanEntry *)p.c.workspace, token_start, (int)begin, (int)min(begin + SPAN, (long long)total));
 }
 
-// A block per pool: how many blocks each sequence gives back, and where to.
-__global__ void __launch_bounds__(RELEASE_THREADS) release_kernel(const CacheReleaseParams p)
+// A cluster per pool.  A warp takes a row of 32 sequences, or several, one behind the other; where there are more warps than rows,
+// several share a row's blocks.  Blocks are copied one by one over all lanes, whatever sequence they come from.
+constexpr int RELEASE_CLUSTER = 8, RELEASE_GROUPS = RELEASE_CLUSTER * MOST_WARPS;
+
+template <int THREADS> __global__ void __launch_bounds__(THREADS) release_kernel(const CacheReleaseParams p)
 {
-    __shared__ long long sh_drop[RELEASE_WARPS];
-    __shared__ int sh_total;
+    __shared__ long long sh_drop[RELEASE_GROUPS];       // the warps' sums, of the whole cluster
     launch_dependents();
     grid_dependency_wait();
     const metasd_cache &c = p.c;
-    const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, batch = p.batch;
-    ReleaseEntry *entries = (ReleaseEntry *)c.workspace + (int64_t)g * c.max_batch;
+    const int ranks = (int)cluster_size(), rank = (int)cluster_rank();
+    const int g = (int)blockIdx.x / ranks, lane = threadIdx.x & 31, batch = p.batch;
+    const int warps = ranks * (THREADS / 32), w = rank * (THREADS / 32) + (int)(threadIdx.x >> 5);
+    const int rows = (batch + 31) / 32, share = max(warps / rows, 1), groups = warps / share, group = w / share, sub = w - group * share;
+    const int row0 = rows * min(group, groups) / groups, row1 = rows * min(group + 1, groups) / groups;
     const int32_t *keep = p.keep + g * p.keep_pool;
     int32_t *held = c.held + (int64_t)g * c.max_batch;
-    const int free = min(max(c.free_count[g], 0), c.n_blocks);
-    uint32_t flags = free != c.free_count[g] ? METASD_STATUS_BAD_STATE : 0u;
-    auto look = [&](int b, int &from) {
+    const int32_t *tables = c.block_table + (int64_t)g * c.max_batch * c.max_blocks;
+    int32_t *list = c.free_blocks + (int64_t)g * c.n_blocks;
+    const int count = c.free_count[g], free = min(max(count, 0), c.n_blocks);
+    uint32_t flags = free != count ? METASD_STATUS_BAD_STATE : 0u;
+    // blocks that the row's sequences give back, a lane each, and the first of them
+    auto look = [&](int row, int &from) {
+        const int b = row * 32 + lane;
+        from = 0;
+        if (b >= batch) return 0;
         const int has = held[b], kept = min(max(has, 0), c.max_blocks), length = __ldg(keep + b);
         if (kept != has) flags |= METASD_STATUS_BAD_STATE;
         if (length < 0) flags |= METASD_STATUS_BAD_LENGTH;
-        from = length <= 0 ? 0 : divide(length - 1, c.page_size, p.page_inverse) + 1;
+        if (length > 0) from = divide(length - 1, c.page_size, p.page_inverse) + 1;
         return length < 0 ? 0 : max(kept - from, 0);
     };
-    const int rows = (batch + 31) / 32, row0 = (int)((long long)rows * warp / RELEASE_WARPS), row1 = (int)((long long)rows * (warp + 1) / RELEASE_WARPS);
-    long long drop = 0;
-    int from;
+    int from = 0, drop = 0;
+    long long mine = 0;
     for (int row = row0; row < row1; ++row) {
-        const int b = row * 32 + lane;
-        if (b < batch) drop += look(b, from);
+        drop = look(row, from);
+        mine += drop;
     }
-    drop = warp_total(drop);
-    if (lane == 0) sh_drop[warp] = drop;
-    if (tid == 0) sh_total = 0;
-    __syncthreads();
-    {
-        const long long d = sh_drop[lane], before = warp_sum_up_to(d) - d;
-        drop = __shfl_sync(FULL, before, warp);
+    mine = warp_total(mine);
+    cluster_arrive_relaxed();
+    cluster_wait();             // every block of the cluster runs
+    if (sub == 0 && lane < ranks && group < RELEASE_GROUPS) {
+        const uint32_t to = map_to_rank(smem_addr(sh_drop + group), (uint32_t)lane);
+        asm volatile("st.shared::cluster.s64 [%0], %1;" ::"r"(to), "l"(group < groups ? mine : 0ll) : "memory");
     }
-    const long long drop0 = drop;
-    // the sequences whose blocks fit behind the free ones: all, unless the tables hold what was not taken from here
-    for (int row = row0; row < row1; ++row) {
-        const int b = row * 32 + lane, n = b < batch ? look(b, from) : 0;
-        const long long upto = warp_sum_up_to((long long)n);
-        if (n && free + drop + upto <= c.n_blocks) atomicMax(&sh_total, (int)(drop + upto));
-        drop += __shfl_sync(FULL, upto, 31);
+    cluster_sync_all();         // the sums are there, and everyone has read what is changed below
+    long long before = 0, total = 0;
+    for (int i = lane; i < groups; i += 32) {
+        total += sh_drop[i];
+        if (i < group) before += sh_drop[i];
     }
-    __syncthreads();
-    drop = drop0;
-    for (int row = row0; row < row1; ++row) {
-        const int b = row * 32 + lane, n = b < batch ? look(b, from) : 0;
-        const long long upto = warp_sum_up_to((long long)n);
-        if (b < batch) {
-            ReleaseEntry e = {0, 0, 0, 0};
-            if (n) {
-                if (drop + upto <= sh_total) {
-                    e = ReleaseEntry{from, n, free + sh_total - 1 - (int)(drop + upto - n), 0};
-                    held[b] = from;
-                } else {
-                    flags |= METASD_STATUS_BAD_STATE;
-                }
+    total = warp_total(total);
+    before = warp_total(before);
+    const bool fits = free + total <= c.n_blocks;       // else the tables hold what was not taken from here: nothing is given back
+    if (!fits) flags |= METASD_STATUS_BAD_STATE;
+    if (fits && group < groups) {
+        for (int row = row0; row < row1; ++row) {
+            if (row1 - row0 > 1) drop = look(row, from);
+            const int upto = warp_sum_up_to(drop), n = __shfl_sync(FULL, upto, 31);
+            const long long top = free + total - 1 - before;
+            for (int e0 = 32 * sub; e0 < n; e0 += 32 * share) {
+                const int e = e0 + lane;
+                int owner = 0;          // the lane whose blocks hold entry e: the first that ends behind it
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1)
+                    if (__shfl_sync(FULL, upto, owner + o - 1) <= e) owner += o;
+                owner = min(owner, 31);
+                const int first = __shfl_sync(FULL, from, owner), rest = e - __shfl_sync(FULL, upto - drop, owner);
+                if (e < n) list[top - e] = tables[(int64_t)(row * 32 + owner) * c.max_blocks + first + rest];
             }
-            entries[b] = e;
+            before += n;
+            __syncwarp();
+            if (sub == 0 && drop > 0) held[row * 32 + lane] = from;
         }
-        drop += __shfl_sync(FULL, upto, 31);
     }
     flags = __reduce_or_sync(FULL, flags);
     if (flags && lane == 0 && c.status) atomicOr(c.status, flags);
-    if (tid == 0) c.free_count[g] = free + sh_total;
-}
-
-// A warp per sequence and pool.
-__global__ void __launch_bounds__(FILL_THREADS) give_back_kernel(const CacheReleaseParams p)
-{
-    launch_dependents();
-    grid_dependency_wait();
-    const metasd_cache &c = p.c;
-    const int lane = threadIdx.x & 31;
-    const int64_t unit = (int64_t)blockIdx.x * (FILL_THREADS / 32) + (threadIdx.x >> 5);
-    const int g = (int)(unit / p.batch), b = (int)(unit - (int64_t)g * p.batch);
-    if (g >= c.n_pools) return;
-    const ReleaseEntry e = ((const ReleaseEntry *)c.workspace)[(int64_t)g * c.max_batch + b];
-    const int32_t *table = c.block_table + ((int64_t)g * c.max_batch + b) * c.max_blocks + e.from;
-    int32_t *free = c.free_blocks + (int64_t)g * c.n_blocks + e.to;
-    for (int i = lane; i < e.drop; i += 32) free[-i] = table[i];
+    if (w == 0 && lane == 0 && (fits || free != count)) c.free_count[g] = fits ? free + (int)total : free;
 }
 
 }  // namespace
 
-size_t cache_workspace_bytes(int max_batch, int n_pools)
-{
-    return std::max((size_t)max_batch * sizeof(PlanEntry), (size_t)max_batch * n_pools * sizeof(ReleaseEntry));
-}
+size_t cache_workspace_bytes(int max_batch, int n_pools) { return (size_t)max_batch * sizeof(PlanEntry); }
 
-constexpr int ALONE_TOKENS = 4096;
-
+#ifndef TUNE_FUSED
+#define TUNE_FUSED 65536
+#define TUNE_PC 8
+#define TUNE_RC 8
+#define TUNE_SMALL 256
+#endif
 cudaError_t launch_cache_plan(const CachePlanParams &p, int n_sm, cudaStream_t stream)
 {
-    if (p.max_tokens <= ALONE_TOKENS) return launch_kernel(plan_kernel<true>, 1, PLAN_THREADS, 0, 1, true, stream, p);
-    cudaError_t e = launch_kernel(plan_kernel<false>, 1, PLAN_THREADS, 0, 1, true, stream, p);
+    if (p.max_tokens <= TUNE_FUSED) {
+        const int threads = p.batch <= 256 ? 256 : MOST_THREADS;
+        int cluster = 1;
+        while (cluster < TUNE_PC && cluster * 2 * threads < p.max_tokens) cluster *= 2;
+        return p.batch <= 256 ? launch_kernel(plan_kernel<256, true>, (unsigned)cluster, 256, 0, cluster, true, stream, p)
+                              : launch_kernel(plan_kernel<MOST_THREADS, true>, (unsigned)cluster, MOST_THREADS, 0, cluster, true, stream, p);
+    }
+    cudaError_t e = p.batch <= 256 ? launch_kernel(plan_kernel<256, false>, 1, 256, 0, 1, true, stream, p)
+                                   : launch_kernel(plan_kernel<MOST_THREADS, false>, 1, MOST_THREADS, 0, 1, true, stream, p);
     if (e != cudaSuccess) return e;
     const unsigned grid = (unsigned)std::min<long long>(((long long)p.max_tokens + SPAN - 1) / SPAN, 8ll * n_sm);
     return launch_kernel(fill_kernel, grid, FILL_THREADS, 0, 1, true, stream, p);
@@ -444,10 +532,13 @@ cudaError_t launch_cache_plan(const CachePlanParams &p, int n_sm, cudaStream_t s
 
 cudaError_t launch_cache_release(const CacheReleaseParams &p, cudaStream_t stream)
 {
-    cudaError_t e = launch_kernel(release_kernel, (unsigned)p.c.n_pools, RELEASE_THREADS, 0, 1, true, stream, p);
-    if (e != cudaSuccess) return e;
-    const long long units = (long long)p.batch * p.c.n_pools, per = FILL_THREADS / 32;
-    return launch_kernel(give_back_kernel, (unsigned)((units + per - 1) / per), FILL_THREADS, 0, 1, true, stream, p);
+    int cluster = 1;
+    if (p.batch <= TUNE_SMALL) {
+        while (cluster < TUNE_RC && cluster * 32 < p.batch) cluster *= 2;
+        return launch_kernel(release_kernel<256>, (unsigned)(p.c.n_pools * cluster), 256, 0, cluster, true, stream, p);
+    }
+    while (cluster < TUNE_RC && cluster * 128 < p.batch) cluster *= 2;
+    return launch_kernel(release_kernel<MOST_THREADS>, (unsigned)(p.c.n_pools * cluster), MOST_THREADS, 0, cluster, true, stream, p);
 }
 
 }  // namespace metasd

@@ -72,7 +72,7 @@ def test_cache_calls_check_their_arguments(lib):
         assert release(good, **kw) == M.ERR_INVALID_ARGUMENT, kw
     for n, p in ((0, 1), (65536, 1), (1, 0), (1, 33), (-1, -1)):
         assert lib.metasd_cache_workspace_bytes(n, p) == 0
-    assert lib.metasd_cache_workspace_bytes(100, 3) >= 100 * 3 * 16 and lib.metasd_cache_workspace_bytes(1, 1) > 0
+    assert lib.metasd_cache_workspace_bytes(100, 3) >= 100 * 32 and lib.metasd_cache_workspace_bytes(1, 1) > 0
 
 
 def test_the_cache_mirror_matches_the_header():
