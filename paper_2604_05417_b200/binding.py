@@ -193,7 +193,7 @@ def _refuse(name: str, t, dtype, shape, index: int):
 
 # The library sees addresses only: what they lead to is checked here.  (dtypes are single objects; get_device() is -1 off CUDA)
 def _expect(name: str, t, dtype, shape, index: int):
-    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous()):
+    if not (t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous()):
         _refuse(name, t, dtype, shape, index)
 
 

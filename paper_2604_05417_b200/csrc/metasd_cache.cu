@@ -7,9 +7,15 @@
 // A sequence whose table is too short takes need = ceil(length / page) - held blocks from the end of its pool's free list, behind
 // what the sequences before it take: running sums again.
 //
-// Two kernels.  The sums are one block's work: it reads some 20 bytes a sequence, and what it costs is the latency of its steps.
-// The entries are spread over the whole GPU and bound by the 16 bytes that are written for each.  A step whose buffers have room
-// for few entries is done by the first kernel alone.
+// Two kernels.  The sums are one block's work: it reads some 20 bytes a sequence, and what it costs is the latency of its steps (4 us
+// for 1024 sequences: two dependent loads 1.1, the sums and what is written for them 2).  The entries are spread over the whole
+// GPU: 16 bytes are written for each, 100 MB for 6.3 M entries in 20 us (5 TB/s; a fill of that size takes 15), and what is
+// left is latency, not instructions: the same walk in two thirds of them takes as long.  A step whose buffers have room for few entries is
+// done by the first kernel alone.
+//
+// A release gives back what lies beyond the entries that stay, to the end of the free list, in the order that lets the next plan
+// take the same blocks for the same places: one cluster per pool, bound by latency too (2.1 us for one sequence, 3.3 for 1024 with
+// nothing to give back, 9 for 98 304 blocks).
 #include <algorithm>
 
 #include "metasd_staged.cuh"
@@ -20,7 +26,7 @@ namespace {
 
 constexpr int MOST_THREADS = 1024, MOST_WARPS = 32;
 constexpr int KEYS = METASD_MAX_POOLS + 1;      // the pools, and who takes no part
-constexpr int FILL_THREADS = 256, SPAN = 2048;  // of the second kernel: entries that a block deals with at once
+constexpr int FILL_THREADS = 256, FILL_BLOCKS = 6;     // of the second kernel; blocks to an SM
 constexpr int STARTS = 2048;                    // places whose first entries a block keeps in shared memory
 constexpr unsigned FULL = 0xFFFFFFFFu;
 
@@ -68,9 +74,19 @@ __device__ __forceinline__ int pool_of(const CachePlanParams &p, int b, uint32_t
     return g < 0 || g >= p.c.n_pools ? p.c.n_pools : g;
 }
 
-// The last place from lo on (token_start[lo] <= t) and in front of hi that starts at or in front of entry t: entry t is its.
-__device__ __forceinline__ int place_of(const int32_t *token_start, int lo, int hi, int t)
+// First entries by place, in shared memory where they fit.
+struct InShared {
+    const int32_t *at;
+    __device__ __forceinline__ int operator[](int i) const { return at[i]; }
+};
+struct InGlobal {
+    const int32_t *at;
+    __device__ __forceinline__ int operator[](int i) const { return __ldcg(at + i); }
+};
+// The last place from lo on (token_start[lo] <= t) that starts at or in front of entry t: entry t is its.
+template <typename Starts> __device__ __forceinline__ int place_of(const Starts &token_start, int lo, int batch, int t)
 {
+    int hi = batch;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (token_start[mid] <= t) lo = mid;
@@ -79,58 +95,104 @@ __device__ __forceinline__ int place_of(const int32_t *token_start, int lo, int 
     return lo;
 }
 
-// Entry t: its slot, position and sequence.  The first entry of a block that is taken writes the block table.
-struct Entry {
-    long long slot;
-    int position, sequence;
-};
-__device__ __forceinline__ Entry entry_at(const CachePlanParams &p, const PlanEntry *entries, const int32_t *token_start, int at, int t)
-{
-    const metasd_cache &c = p.c;
-    const PlanEntry e = entries[at];
-    Entry r;
-    r.sequence = e.sequence;
-    r.position = e.cached + (t - token_start[at]);
-    r.slot = -1;
-    if (e.first != -1) {
-        const int block = divide(r.position, c.page_size, p.page_inverse), in = r.position - block * c.page_size;
-        int32_t *table = c.block_table + ((int64_t)e.pool * c.max_batch + e.sequence) * c.max_blocks;
-        int id;
-        if (block >= e.held) {
-            id = c.free_blocks[(int64_t)e.pool * c.n_blocks + (e.first - (block - e.held))];
-            if (in == 0) table[block] = id;
-        } else {
-            id = table[block];
-        }
-        r.slot = (long long)id * c.page_size + in;
+// The entries of one place.  The first entry of a block that is taken writes the block table.
+struct Place {
+    int sequence, cached, held;
+    bool planned;
+    int32_t *table;             // the sequence's row of the block table
+    const int32_t *taken;       // taken[-block]: block `block` of the row, where it is taken from the free list
+
+    __device__ __forceinline__ void at(const CachePlanParams &p, const PlanEntry &e)
+    {
+        sequence = e.sequence;
+        cached = e.cached;
+        held = e.held;
+        planned = e.first != -1;
+        table = p.c.block_table + ((int64_t)e.pool * p.c.max_batch + e.sequence) * p.c.max_blocks;
+        taken = p.c.free_blocks + (int64_t)e.pool * p.c.n_blocks + (e.held + e.first);
     }
-    return r;
+    __device__ __forceinline__ int id(int block) const { return planned ? *(block >= held ? taken - block : table + block) : 0; }
+    __device__ __forceinline__ void note(int block, int id) const
+    {
+        if (planned && block >= held) table[block] = id;
+    }
+    __device__ __forceinline__ long long slot(const CachePlanParams &p, int id, int in) const
+    {
+        return planned ? (long long)id * p.c.page_size + in : -1;
+    }
+};
+
+// Two entries that lie next to each other.
+struct Two {
+    long long slot, slot1;
+    int position, position1, sequence, sequence1;
+};
+__device__ __forceinline__ void put(const CachePlanParams &p, int t, int end, const Two &e)
+{
+    if (p.wide && t + 1 < end) {
+        *reinterpret_cast<longlong2 *>(p.slot_map + t) = make_longlong2(e.slot, e.slot1);
+        if (p.position) *reinterpret_cast<int2 *>(p.position + t) = make_int2(e.position, e.position1);
+        if (p.sequence) *reinterpret_cast<int2 *>(p.sequence + t) = make_int2(e.sequence, e.sequence1);
+        return;
+    }
+    p.slot_map[t] = e.slot;
+    if (p.position) p.position[t] = e.position;
+    if (p.sequence) p.sequence[t] = e.sequence;
+    if (t + 1 >= end) return;
+    p.slot_map[t + 1] = e.slot1;
+    if (p.position) p.position[t + 1] = e.position1;
+    if (p.sequence) p.sequence[t + 1] = e.sequence1;
 }
 
-// Entries begin .. end - 1, by one block, two to a thread.
-template <int THREADS>
-__device__ __forceinline__ void fill(const CachePlanParams &p, const PlanEntry *entries, const int32_t *token_start, int begin, int end)
+// Entries begin .. end - 1, by one block, two to a thread at a time; a thread's next two are often of the same sequence.
+template <int THREADS, typename Starts>
+__device__ __forceinline__ void fill(const CachePlanParams &p, const PlanEntry *entries, const Starts &token_start, int begin, int end)
 {
-    const int lo = place_of(token_start, 0, p.batch, begin), hi = place_of(token_start, lo, p.batch, end - 1) + 1;
-    for (int t = begin + 2 * (int)threadIdx.x; t < end; t += 2 * THREADS) {
-        const int at = place_of(token_start, lo, hi, t);
-        const Entry a = entry_at(p, entries, token_start, at, t);
+    Place x;
+    int from = 0, to = 0, at = 0;       // the entries of the place
+    const int page = p.c.page_size;
+    auto find = [&](int t) {
+        at = place_of(token_start, at, p.batch, t);
+        from = token_start[at];
+        to = token_start[at + 1];
+        x.at(p, entries[at]);
+    };
+    auto split = [&](int position, int &block, int &in) {
+        block = divide(position, page, p.page_inverse);
+        in = position - block * page;
+    };
+    for (long long next = begin + 2 * (int)threadIdx.x; next < end; next += 2 * THREADS) {
+        const int t = (int)next;
+        if (t >= to) find(t);
+        Two e;
+        int block, in;
+        e.position = x.cached + (t - from);
+        e.sequence = x.sequence;
+        split(e.position, block, in);
+        int id = x.id(block);
+        if (in == 0) x.note(block, id);
+        e.slot = x.slot(p, id, in);
+        e.slot1 = 0;
+        e.position1 = e.sequence1 = 0;
         if (t + 1 < end) {
-            const int next = token_start[at + 1] > t + 1 ? at : place_of(token_start, at + 1, hi, t + 1);
-            const Entry b = entry_at(p, entries, token_start, next, t + 1);
-            if (p.wide) {
-                *reinterpret_cast<longlong2 *>(p.slot_map + t) = make_longlong2(a.slot, b.slot);
-                if (p.position) *reinterpret_cast<int2 *>(p.position + t) = make_int2(a.position, b.position);
-                if (p.sequence) *reinterpret_cast<int2 *>(p.sequence + t) = make_int2(a.sequence, b.sequence);
-                continue;
+            if (t + 1 >= to) {
+                find(t + 1);
+                e.position1 = x.cached;
+                split(e.position1, block, in);
+                id = x.id(block);
+            } else {
+                e.position1 = e.position + 1;
+                if (++in == page) {
+                    ++block;
+                    in = 0;
+                    id = x.id(block);
+                }
             }
-            p.slot_map[t + 1] = b.slot;
-            if (p.position) p.position[t + 1] = b.position;
-            if (p.sequence) p.sequence[t + 1] = b.sequence;
+            if (in == 0) x.note(block, id);
+            e.sequence1 = x.sequence;
+            e.slot1 = x.slot(p, id, in);
         }
-        p.slot_map[t] = a.slot;
-        if (p.position) p.position[t] = a.position;
-        if (p.sequence) p.sequence[t] = a.sequence;
+        put(p, t, end, e);
     }
 }
 
@@ -205,7 +267,7 @@ template <int THREADS> __device__ __forceinline__ void look_at_pools(const Cache
 }
 
 // Order, running sums and the block tables' growth of a step, by one block with a sequence (then a place) per thread, in registers
-// and shared memory.
+// and shared memory; the blocks of all tables together are fewer than 2^31.
 template <int THREADS> __device__ __forceinline__ void plan_step(const CachePlanParams &p, PlanShared<THREADS> &sh)
 {
     constexpr int WARPS = THREADS / 32;
@@ -250,22 +312,22 @@ template <int THREADS> __device__ __forceinline__ void plan_step(const CachePlan
     }
     // running sums of the entries and of the blocks
     const uint32_t tokens = in ? (uint32_t)e.fresh : 0u, upto_tokens = warp_add_up_to(tokens);
-    const long long need = in ? e.need : 0, upto_need = warp_sum_up_to(need);
+    const int need = in ? e.need : 0, upto_need = warp_sum_up_to(need);      // p.narrow: they fit
     if (lane == 31) { sh.tokens[warp] = upto_tokens; sh.need[warp] = upto_need; }
     __syncthreads();
     const uint32_t tokens_w = warp_add_up_to(lane < WARPS ? sh.tokens[lane] : 0u);
-    const long long need_w = warp_sum_up_to(lane < WARPS ? sh.need[lane] : 0ll);
+    const int need_w = warp_sum_up_to(lane < WARPS ? (int)sh.need[lane] : 0);
     uint32_t tokens0 = __shfl_sync(FULL, tokens_w, (warp + 31) & 31), before_lane = __shfl_up_sync(FULL, upto_tokens, 1);
-    long long need0 = __shfl_sync(FULL, need_w, (warp + 31) & 31);
+    int need0 = __shfl_sync(FULL, need_w, (warp + 31) & 31);
     if (warp == 0) { tokens0 = 0u; need0 = 0; }
     if (lane == 0) before_lane = 0u;
-    const long long blocks = need0 + upto_need - need;
+    const int blocks = need0 + upto_need - need;
     if (p.pool) {
         if (in && e.leads) sh.base[e.pool] = blocks;
         __syncthreads();
     }
     if (in) {
-        serve(p, sh, e, tid, add_up(tokens0, before_lane), p.pool && e.fresh ? blocks - sh.base[e.pool] : blocks, flags);
+        serve(p, sh, e, tid, add_up(tokens0, before_lane), p.pool && e.fresh ? blocks - (int)sh.base[e.pool] : blocks, flags);
         sh.entries[tid] = e;
         ((PlanEntry *)p.c.workspace)[tid] = e;
     }
@@ -275,7 +337,7 @@ template <int THREADS> __device__ __forceinline__ void plan_step(const CachePlan
     for (int i = tid; i < P; i += THREADS) p.c.free_count[i] = sh.free[i] - sh.taken[i];
 }
 
-// The same for more sequences than a block has threads: a warp takes rows of 32, one behind the other, through the workspace.
+// The same for any number of sequences and blocks: a warp takes rows of 32, one behind the other, through the workspace.
 __device__ __forceinline__ void plan_rows(const CachePlanParams &p, PlanShared<MOST_THREADS> &sh)
 {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, batch = p.batch, P = p.c.n_pools;
@@ -383,7 +445,7 @@ template <int THREADS, bool FILLS> __global__ void __launch_bounds__(THREADS) pl
     const int rank = FILLS ? (int)cluster_rank() : 0, batch = p.batch;
     if (rank == 0) {
         if constexpr (THREADS == MOST_THREADS) {
-            if (batch <= THREADS) plan_step<THREADS>(p, sh);
+            if (p.narrow && batch <= THREADS) plan_step<THREADS>(p, sh);
             else plan_rows(p, sh);
         } else {
             plan_step<THREADS>(p, sh);
@@ -392,41 +454,45 @@ template <int THREADS, bool FILLS> __global__ void __launch_bounds__(THREADS) pl
     if constexpr (FILLS) {
         const int ranks = (int)cluster_size();
         if (ranks > 1) cluster_sync_all();
-        const int32_t *token_start = p.token_start;
-        const PlanEntry *entries = (const PlanEntry *)p.c.workspace;
-        if (batch <= STARTS) {
-            if (rank != 0) {
-                for (int i = threadIdx.x; i <= batch; i += THREADS) sh.token_start[i] = __ldcg(p.token_start + i);
-                __syncthreads();
-            }
-            token_start = sh.token_start;
+        const bool near = batch <= STARTS;
+        if (near && rank != 0) {
+            for (int i = threadIdx.x; i <= batch; i += THREADS) sh.token_start[i] = __ldcg(p.token_start + i);
+            __syncthreads();
         }
-        if (rank == 0 && batch <= THREADS) entries = sh.entries;
-        const int total = min(token_start[batch], p.max_tokens), share = 2 * THREADS;
-        for (long long begin = (long long)share * rank; begin < total; begin += (long long)share * ranks)
-            fill<THREADS>(p, entries, token_start, (int)begin, (int)min(begin + share, (long long)total));
+        const PlanEntry *entries = rank == 0 && p.narrow && batch <= THREADS ? sh.entries : (const PlanEntry *)p.c.workspace;
+        const int total = min(near ? sh.token_start[batch] : __ldcg(p.token_start + batch), p.max_tokens), share = 2 * THREADS;
+        for (long long begin = (long long)share * rank; begin < total; begin += (long long)share * ranks) {
+            const int end = (int)min(begin + share, (long long)total);
+            if (near) fill<THREADS>(p, entries, InShared{sh.token_start}, (int)begin, end);
+            else fill<THREADS>(p, entries, InGlobal{p.token_start}, (int)begin, end);
+        }
     }
 }
 
-__global__ void __launch_bounds__(FILL_THREADS) fill_kernel(const CachePlanParams p)
+// Each block a stretch of its own, of the entries that there are: one search and a walk.
+__global__ void __launch_bounds__(FILL_THREADS, FILL_BLOCKS) fill_kernel(const CachePlanParams p)
 {
     __shared__ int32_t sh_start[STARTS + 1];
     launch_dependents();
     grid_dependency_wait();
-    const int32_t *token_start = p.token_start;
-    if (p.batch <= STARTS) {
+    const PlanEntry *entries = (const PlanEntry *)p.c.workspace;
+    const bool near = p.batch <= STARTS;
+    const int total = min(__ldcg(p.token_start + p.batch), p.max_tokens);
+    const long long turn = 2 * FILL_THREADS, turns = (total + turn - 1) / turn, each = (turns + gridDim.x - 1) / gridDim.x * turn;
+    const long long begin = each * blockIdx.x;
+    if (begin >= total) return;
+    if (near) {
         for (int i = threadIdx.x; i <= p.batch; i += FILL_THREADS) sh_start[i] = __ldcg(p.token_start + i);
         __syncthreads();
-        token_start = sh_start;
     }
-    const int total = min(token_start[p.batch], p.max_tokens);
-    for (long long begin = (long long)blockIdx.x * SPAN; begin < total; begin += (long long)gridDim.x * SPAN)
-        fill<FILL_THREADS>(p, (const PlanEntry *)p.c.workspace, token_start, (int)begin, (int)min(begin + SPAN, (long long)total));
+    const int end = (int)min(begin + each, (long long)total);
+    if (near) fill<FILL_THREADS>(p, entries, InShared{sh_start}, (int)begin, end);
+    else fill<FILL_THREADS>(p, entries, InGlobal{p.token_start}, (int)begin, end);
 }
 
 // A cluster per pool.  A warp takes a row of 32 sequences, or several, one behind the other; where there are more warps than rows,
 // several share a row's blocks.  Blocks are copied one by one over all lanes, whatever sequence they come from.
-constexpr int RELEASE_CLUSTER = 8, RELEASE_GROUPS = RELEASE_CLUSTER * MOST_WARPS;
+constexpr int RELEASE_CLUSTER = 8, RELEASE_GROUPS = RELEASE_CLUSTER * MOST_WARPS, AT_ONCE = 4;
 
 template <int THREADS> __global__ void __launch_bounds__(THREADS) release_kernel(const CacheReleaseParams p)
 {
@@ -437,8 +503,10 @@ template <int THREADS> __global__ void __launch_bounds__(THREADS) release_kernel
     const int ranks = (int)cluster_size(), rank = (int)cluster_rank();
     const int g = (int)blockIdx.x / ranks, lane = threadIdx.x & 31, batch = p.batch;
     const int warps = ranks * (THREADS / 32), w = rank * (THREADS / 32) + (int)(threadIdx.x >> 5);
-    const int rows = (batch + 31) / 32, share = max(warps / rows, 1), groups = warps / share, group = w / share, sub = w - group * share;
-    const int row0 = rows * min(group, groups) / groups, row1 = rows * min(group + 1, groups) / groups;
+    // p.share warps to a row, or p.share == 0 and several rows to a warp
+    const int rows = (batch + 31) / 32, share = max(p.share, 1), group = p.share > 1 ? divide(w, share, p.share_inverse) : w, sub = w - group * share;
+    const int groups = p.share ? min(rows, warps) : warps, each = p.share ? 1 : (rows + warps - 1) / warps;
+    const int row0 = min(group * each, rows), row1 = min(row0 + each, rows);
     const int32_t *keep = p.keep + g * p.keep_pool;
     int32_t *held = c.held + (int64_t)g * c.max_batch;
     const int32_t *tables = c.block_table + (int64_t)g * c.max_batch * c.max_blocks;
@@ -465,9 +533,9 @@ template <int THREADS> __global__ void __launch_bounds__(THREADS) release_kernel
     mine = warp_total(mine);
     cluster_arrive_relaxed();
     cluster_wait();             // every block of the cluster runs
-    if (sub == 0 && lane < ranks && group < RELEASE_GROUPS) {
+    if (sub == 0 && lane < ranks && group < groups) {
         const uint32_t to = map_to_rank(smem_addr(sh_drop + group), (uint32_t)lane);
-        asm volatile("st.shared::cluster.s64 [%0], %1;" ::"r"(to), "l"(group < groups ? mine : 0ll) : "memory");
+        asm volatile("st.shared::cluster.s64 [%0], %1;" ::"r"(to), "l"(mine) : "memory");
     }
     cluster_sync_all();         // the sums are there, and everyone has read what is changed below
     long long before = 0, total = 0;
@@ -484,15 +552,24 @@ template <int THREADS> __global__ void __launch_bounds__(THREADS) release_kernel
             if (row1 - row0 > 1) drop = look(row, from);
             const int upto = warp_sum_up_to(drop), n = __shfl_sync(FULL, upto, 31);
             const long long top = free + total - 1 - before;
-            for (int e0 = 32 * sub; e0 < n; e0 += 32 * share) {
-                const int e = e0 + lane;
-                int owner = 0;          // the lane whose blocks hold entry e: the first that ends behind it
+            for (int e0 = 32 * sub; e0 < n; e0 += 32 * share * AT_ONCE) {
+                int id[AT_ONCE];
 #pragma unroll
-                for (int o = 16; o > 0; o >>= 1)
-                    if (__shfl_sync(FULL, upto, owner + o - 1) <= e) owner += o;
-                owner = min(owner, 31);
-                const int first = __shfl_sync(FULL, from, owner), rest = e - __shfl_sync(FULL, upto - drop, owner);
-                if (e < n) list[top - e] = tables[(int64_t)(row * 32 + owner) * c.max_blocks + first + rest];
+                for (int i = 0; i < AT_ONCE; ++i) {
+                    const int e = e0 + 32 * share * i + lane;
+                    int owner = 0;          // the lane whose blocks hold entry e: the first that ends behind it
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1)
+                        if (__shfl_sync(FULL, upto, owner + o - 1) <= e) owner += o;
+                    owner = min(owner, 31);
+                    const int place = __shfl_sync(FULL, from - (upto - drop), owner) + e;
+                    id[i] = e < n ? tables[(int64_t)(row * 32 + owner) * c.max_blocks + place] : 0;
+                }
+#pragma unroll
+                for (int i = 0; i < AT_ONCE; ++i) {
+                    const int e = e0 + 32 * share * i + lane;
+                    if (e < n) list[top - e] = id[i];
+                }
             }
             before += n;
             __syncwarp();
@@ -508,37 +585,45 @@ template <int THREADS> __global__ void __launch_bounds__(THREADS) release_kernel
 
 size_t cache_workspace_bytes(int max_batch, int n_pools) { return (size_t)max_batch * sizeof(PlanEntry); }
 
-#ifndef TUNE_FUSED
-#define TUNE_FUSED 65536
-#define TUNE_PC 8
-#define TUNE_RC 8
-#define TUNE_SMALL 256
-#endif
-cudaError_t launch_cache_plan(const CachePlanParams &p, int n_sm, cudaStream_t stream)
+// Up to so many entries (that the outputs have room for) the planning cluster writes them too.  Us a plan and release on the device with one
+// launch and with two, and the entries there is room for and there are: one sequence, 64 and 3, 4.8 and 6.5; 1024 sequences, 9216 and 5 k,
+// 12.2 and 12.2; 333 sequences, 62 k and 16 k, 12.7 and 11.1; 256 sequences, 87 k and 26 k, 16.4 and 10.9.  A launch takes the host
+// 2.2 us.
+constexpr int ALONE_ENTRIES = 65536, PLAN_CLUSTER = 8;
+// Releases of so many sequences take blocks of 256 threads, of more 1024: fewer warps are quicker where little comes back (1024
+// sequences, 11.5 us a plan and release instead of 12.4), more where much does (1024 x 96 blocks: 38 us instead of 47).
+constexpr int SMALL_RELEASE = 512;
+
+cudaError_t launch_cache_plan(const CachePlanParams &params, int n_sm, cudaStream_t stream)
 {
-    if (p.max_tokens <= TUNE_FUSED) {
-        const int threads = p.batch <= 256 ? 256 : MOST_THREADS;
+    CachePlanParams p = params;
+    p.narrow = (long long)p.batch * p.c.max_blocks < (1ll << 31);
+    const bool small = p.narrow && p.batch <= 256;
+    if (p.max_tokens <= ALONE_ENTRIES) {
+        const int threads = small ? 256 : MOST_THREADS;
         int cluster = 1;
-        while (cluster < TUNE_PC && cluster * 2 * threads < p.max_tokens) cluster *= 2;
-        return p.batch <= 256 ? launch_kernel(plan_kernel<256, true>, (unsigned)cluster, 256, 0, cluster, true, stream, p)
-                              : launch_kernel(plan_kernel<MOST_THREADS, true>, (unsigned)cluster, MOST_THREADS, 0, cluster, true, stream, p);
+        while (cluster < PLAN_CLUSTER && cluster * 2 * threads < p.max_tokens) cluster *= 2;
+        return small ? launch_kernel(plan_kernel<256, true>, (unsigned)cluster, 256, 0, cluster, true, stream, p)
+                     : launch_kernel(plan_kernel<MOST_THREADS, true>, (unsigned)cluster, MOST_THREADS, 0, cluster, true, stream, p);
     }
-    cudaError_t e = p.batch <= 256 ? launch_kernel(plan_kernel<256, false>, 1, 256, 0, 1, true, stream, p)
-                                   : launch_kernel(plan_kernel<MOST_THREADS, false>, 1, MOST_THREADS, 0, 1, true, stream, p);
+    cudaError_t e = small ? launch_kernel(plan_kernel<256, false>, 1, 256, 0, 1, true, stream, p)
+                          : launch_kernel(plan_kernel<MOST_THREADS, false>, 1, MOST_THREADS, 0, 1, true, stream, p);
     if (e != cudaSuccess) return e;
-    const unsigned grid = (unsigned)std::min<long long>(((long long)p.max_tokens + SPAN - 1) / SPAN, 8ll * n_sm);
+    const unsigned grid = (unsigned)std::min<long long>(((long long)p.max_tokens + 2 * FILL_THREADS - 1) / (2 * FILL_THREADS), (long long)FILL_BLOCKS * n_sm);
     return launch_kernel(fill_kernel, grid, FILL_THREADS, 0, 1, true, stream, p);
 }
 
-cudaError_t launch_cache_release(const CacheReleaseParams &p, cudaStream_t stream)
+cudaError_t launch_cache_release(const CacheReleaseParams &params, cudaStream_t stream)
 {
+    CacheReleaseParams p = params;
+    const int rows = (p.batch + 31) / 32;
+    const bool small = p.batch <= SMALL_RELEASE;
     int cluster = 1;
-    if (p.batch <= TUNE_SMALL) {
-        while (cluster < TUNE_RC && cluster * 32 < p.batch) cluster *= 2;
-        return launch_kernel(release_kernel<256>, (unsigned)(p.c.n_pools * cluster), 256, 0, cluster, true, stream, p);
-    }
-    while (cluster < TUNE_RC && cluster * 128 < p.batch) cluster *= 2;
-    return launch_kernel(release_kernel<MOST_THREADS>, (unsigned)(p.c.n_pools * cluster), MOST_THREADS, 0, cluster, true, stream, p);
+    while (cluster < RELEASE_CLUSTER && cluster * (small ? 32 : 128) < p.batch) cluster *= 2;
+    p.share = cluster * (small ? 8 : MOST_WARPS) / rows;
+    p.share_inverse = inverse_of((uint32_t)std::max(p.share, 1));
+    return small ? launch_kernel(release_kernel<256>, (unsigned)(p.c.n_pools * cluster), 256, 0, cluster, true, stream, p)
+                 : launch_kernel(release_kernel<MOST_THREADS>, (unsigned)(p.c.n_pools * cluster), MOST_THREADS, 0, cluster, true, stream, p);
 }
 
 }  // namespace metasd

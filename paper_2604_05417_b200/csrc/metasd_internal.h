@@ -137,6 +137,7 @@ struct CachePlanParams {
     int32_t batch, max_tokens;
     uint32_t page_inverse;    // inverse_of(page_size)
     int32_t wide;             // entries may be written in pairs
+    int32_t narrow;           // batch * max_blocks is below 2^31; set by the launcher
     const int32_t *pool, *cached, *length;
     int64_t cached_pool;
     int32_t *order, *place, *pool_start, *token_start;
@@ -147,6 +148,8 @@ struct CacheReleaseParams {
     metasd_cache c;
     int32_t batch;
     uint32_t page_inverse;
+    int32_t share;            // warps to a row of 32 sequences, 0: several rows to a warp; set by the launcher
+    uint32_t share_inverse;
     const int32_t *keep;
     int64_t keep_pool;
 };
