@@ -192,20 +192,37 @@ def _refuse(name: str, t, dtype, shape, index: int):
 
 
 # The library sees addresses only: what they lead to is checked here.  (dtypes are single objects; get_device() is -1 off CUDA)
+def _are(index: int, dtype, shape, *tensors) -> bool:
+    """Whether all tensors, None aside, are contiguous ones of this device, type and shape."""
+    return all(t is None or (t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous()) for t in tensors)
+
+
 def _expect(name: str, t, dtype, shape, index: int):
-    if not (t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous()):
+    if t is None or not _are(index, dtype, shape, t):
         _refuse(name, t, dtype, shape, index)
+
+
+def _expect_all(index: int, dtype, shape, **tensors):
+    """Names the tensor that is not what is due."""
+    for name, t in tensors.items():
+        if t is not None:
+            _expect(name, t, dtype, shape, index)
 
 
 def _verify_probs(ctx, target, draft, tokens, u_accept, u_draw, draft_len, draft_place, seed, out, want_d_tv, status):
     dtype, index = target.dtype, target.get_device()
     if index < 0 or target.dim() != 3 or (dtype is not torch.float32 and dtype is not torch.bfloat16):
         raise ValueError("target_probs: a CUDA tensor [B, k + 1, V] of bf16 or fp32 is due")
+    lib = _lib or load_library()
+    are = _are if _call is None else _call.are
     B, rows, V = target.shape
-    k, i32, f32, per_sequence = rows - 1, torch.int32, torch.float32, (B,)
+    k, i32, f32, each = rows - 1, torch.int32, torch.float32, (B,)
     tss, trs, entry = target.stride()
     if entry != 1 and V > 1:
         raise ValueError("target_probs: a row's entries have to lie next to each other (stride %d)" % entry)
+    if out is None:
+        out = ProbsResult(torch.empty(each, dtype=i32, device=target.device), torch.empty(each, dtype=i32, device=target.device))
+    accepted, token, d_tv, reward = out.accepted_len, out.next_token, None, None
     dss = drs = 0
     if k > 0:
         drafted = (B, k)
@@ -215,41 +232,35 @@ def _verify_probs(ctx, target, draft, tokens, u_accept, u_draw, draft_len, draft
             dss, drs, entry = draft.stride()
             if entry != 1 and V > 1:
                 raise ValueError("draft_probs: a row's entries have to lie next to each other (stride %d)" % entry)
-        _expect("draft_tokens", tokens, i32, drafted, index)
-        _expect("u_accept", u_accept, f32, drafted, index)
+        if want_d_tv:
+            d_tv = out.d_tv
+            if d_tv is None:
+                d_tv = out.d_tv = torch.zeros(drafted, dtype=f32, device=target.device)
+        if tokens is None or not are(index, i32, drafted, tokens):
+            _refuse("draft_tokens", tokens, i32, drafted, index)
+        if u_accept is None or not are(index, f32, drafted, u_accept, d_tv):
+            _expect("u_accept", u_accept, f32, drafted, index)
+            _refuse("d_tv", d_tv, f32, drafted, index)
     else:
         tokens = u_accept = draft = None
-    _expect("u_draw", u_draw, f32, per_sequence, index)
-    if draft_len is not None:
-        _expect("draft_len", draft_len, i32, per_sequence, index)
-    if draft_place is not None:
-        _expect("draft_place", draft_place, i32, per_sequence, index)
+        if want_d_tv and out.d_tv is None:
+            out.d_tv = torch.zeros((B, 0), dtype=f32, device=target.device)
+    if ctx is not None:
+        reward = out.reward
+        if reward is None:
+            reward = out.reward = torch.empty(each, dtype=f32, device=target.device)
+    if u_draw is None or not are(index, f32, each, u_draw, reward):
+        _expect("u_draw", u_draw, f32, each, index)
+        _refuse("reward", reward, f32, each, index)
+    if accepted is None or token is None or not are(index, i32, each, accepted, token, draft_len, draft_place):
+        _expect("accepted_len", accepted, i32, each, index)
+        _expect("next_token", token, i32, each, index)
+        _expect_all(index, i32, each, draft_len=draft_len, draft_place=draft_place)
     if status is not None:
         _expect("status", status, i32, (1,), index)
-    if out is None:
-        out = ProbsResult(torch.empty_like(u_draw, dtype=i32), torch.empty_like(u_draw, dtype=i32))
-    else:
-        _expect("accepted_len", out.accepted_len, i32, per_sequence, index)
-        _expect("next_token", out.next_token, i32, per_sequence, index)
-    d_tv = None
-    if want_d_tv:
-        if out.d_tv is None:
-            out.d_tv = torch.zeros((B, k), dtype=f32, device=target.device)
-        else:
-            _expect("d_tv", out.d_tv, f32, (B, k), index)
-        if k > 0:
-            d_tv = out.d_tv
-    reward = None
-    if ctx is not None:
-        if out.reward is None:
-            out.reward = torch.empty_like(u_draw)
-        else:
-            _expect("reward", out.reward, f32, per_sequence, index)
-        reward = out.reward
-    lib = _lib or load_library()
     stream = _raw_stream(index) if _raw_stream is not None else _stream(target.device)
     args = (ctx, index, B, k, V, BF16 if dtype is torch.bfloat16 else FP32, target, tss, trs, draft, dss, drs, draft_place, tokens, draft_len,
-            u_accept, u_draw, seed, out.accepted_len, out.next_token, d_tv, reward, status, stream)
+            u_accept, u_draw, seed, accepted, token, d_tv, reward, status, stream)
     rc = NotImplemented
     if _call is not None:
         rc = _call.verify_probs(lib.verify_probs_at, *args)
@@ -493,28 +504,14 @@ class BlockCache:
                    torch.zeros((n_pools, max_batch), dtype=i32, device=dev), free,
                    torch.full((n_pools,), n_blocks, dtype=i32, device=dev), page_size)
 
-    def _per_pool(self, name: str, t: torch.Tensor, B: int) -> int:
-        """Entries between pools: of a [B] tensor (the same for all) or an [n_pools, B] one."""
-        if t.dim() == 1:
-            _expect(name, t, torch.int32, (B,), self.index)
-            return 0
-        _expect(name, t, torch.int32, (self.n_pools, B), self.index)
-        return B
-
-    def _stream(self) -> int:
-        return _raw_stream(self.index) if _raw_stream is not None else _stream(self.device)
-
     def plan(self, length: torch.Tensor, cached: torch.Tensor, pool: Optional[torch.Tensor] = None,
              max_tokens: Optional[int] = None, out: Optional[CachePlan] = None) -> CachePlan:
         """metasd_cache_plan: length [B], cached [B] or [n_pools, B], pool [B] (None: pool 0), int32.  max_tokens: entries that the
         outputs have room for, where they are not given."""
         index, i32 = self.index, torch.int32
+        are = _are if _call is None else _call.are
         B = length.shape[0]
         each = (B,)
-        _expect("length", length, i32, each, index)
-        stride = self._per_pool("cached", cached, B)
-        if pool is not None:
-            _expect("pool", pool, i32, each, index)
         if out is None:
             if max_tokens is None:
                 raise ValueError("max_tokens or the outputs are due")
@@ -522,26 +519,25 @@ class BlockCache:
                 return torch.empty(shape, dtype=i32, device=self.device)
             out = CachePlan(ints(B), ints(B), ints(self.n_pools + 1), ints(B + 1),
                             torch.empty(max_tokens, dtype=torch.int64, device=self.device), ints(max_tokens), ints(max_tokens))
-        else:
-            slot_map = out.slot_map
-            room = slot_map.shape[0]
-            if max_tokens is not None and max_tokens != room:
-                raise ValueError("slot_map has room for %d entries, not %d" % (room, max_tokens))
-            max_tokens = room
+        order, place, pool_start, token_start = out.order, out.place, out.pool_start, out.token_start
+        slot_map, position, sequence = out.slot_map, out.position, out.sequence
+        room = slot_map.shape[0]
+        if max_tokens is not None and max_tokens != room:
+            raise ValueError("slot_map has room for %d entries, not %d" % (room, max_tokens))
+        stride = 0 if cached.dim() == 1 else B
+        # one question for each type and shape; who is not what is due is found where the answer is no
+        if not (are(index, i32, each, length, pool, order, place, None if stride else cached) and
+                (stride == 0 or are(index, i32, (self.n_pools, B), cached)) and are(index, i32, (B + 1,), token_start) and
+                token_start is not None and are(index, torch.int64, (room,), slot_map) and are(index, i32, (room,), position, sequence) and
+                are(index, i32, (self.n_pools + 1,), pool_start)):
+            _expect_all(index, i32, each, length=length, pool=pool, order=order, place=place)
+            _expect("cached", cached, i32, (self.n_pools, B) if stride else each, index)
+            _expect("token_start", token_start, i32, (B + 1,), index)
             _expect("slot_map", slot_map, torch.int64, (room,), index)
-            _expect("token_start", out.token_start, i32, (B + 1,), index)
-            if out.order is not None:
-                _expect("order", out.order, i32, each, index)
-            if out.place is not None:
-                _expect("place", out.place, i32, each, index)
-            if out.pool_start is not None:
-                _expect("pool_start", out.pool_start, i32, (self.n_pools + 1,), index)
-            if out.position is not None:
-                _expect("position", out.position, i32, (room,), index)
-            if out.sequence is not None:
-                _expect("sequence", out.sequence, i32, (room,), index)
-        args = (self._at, B, pool, cached, stride, length, max_tokens, out.order, out.place, out.pool_start, out.token_start, out.slot_map,
-                out.position, out.sequence, self._stream())
+            _expect_all(index, i32, (room,), position=position, sequence=sequence)
+            _expect_all(index, i32, (self.n_pools + 1,), pool_start=pool_start)
+        args = (self._at, B, pool, cached, stride, length, room, order, place, pool_start, token_start, slot_map, position, sequence,
+                _raw_stream(index) if _raw_stream is not None else _stream(self.device))
         rc = NotImplemented
         if _call is not None:
             rc = _call.cache_plan(self.lib.cache_plan_at, *args)
@@ -553,8 +549,12 @@ class BlockCache:
 
     def release(self, keep: torch.Tensor):
         """metasd_cache_release: keep [B] (all pools) or [n_pools, B] int32, the entries that stay."""
-        B = keep.shape[-1]
-        args = (self._at, B, keep, self._per_pool("keep", keep, B), self._stream())
+        index, B = self.index, keep.shape[-1]
+        stride = 0 if keep.dim() == 1 else B
+        shape = (self.n_pools, B) if stride else (B,)
+        if not (_are if _call is None else _call.are)(index, torch.int32, shape, keep):
+            _refuse("keep", keep, torch.int32, shape, index)
+        args = (self._at, B, keep, stride, _raw_stream(index) if _raw_stream is not None else _stream(self.device))
         rc = NotImplemented
         if _call is not None:
             rc = _call.cache_release(self.lib.cache_release_at, *args)
