@@ -8,15 +8,17 @@ produces the same quantities for the synthetic workloads, whose generator knows 
 sequence in every round.  Every round runs through the library (C ABI, CUDA kernels); what is computed here is
 bookkeeping on its outputs: means, variances, counts.
 
-    python -m paper_2604_05417_b200.study --workload cfg2_nonstationary --rounds 300 [--bandits ucb,ducb]
+    python -m paper_2604_05417_b200.study --workload cfg2_nonstationary --rounds 300 [--bandits ucb,ducb] [--serve 100]
 
-prints one JSON object and a table.
+prints one JSON object and a table.  With --serve it also runs rounds as a serving loop does, from probabilities that are cut (min-p) and random
+numbers of its own, with the paged caches of the target and of every drafter: how many entries the drafters' caches
+have to catch up with when the bandit moves (the paper's switching cost), and how many blocks the caches hold.
 """
 from __future__ import annotations
 
 import argparse
 import json
-from typing import Dict, List, Sequence
+from typing import Dict, List, Optional, Sequence
 
 import numpy as np
 import torch
@@ -143,6 +145,94 @@ def bandit_run(wl: Workload, rounds: int, reward: int, bandit: str, device=0, se
                 var_be=be.var, be_zero_ratio=zero / be.n, block_efficiency=1.0 + acc.mean, status=status)
 
 
+def cut_probabilities(logits: torch.Tensor, temperature: float, min_p: float) -> torch.Tensor:
+    """softmax(logits / T) in fp32 without the entries below min_p times the row's largest (min-p sampling)."""
+    p = torch.softmax(logits.float() / temperature, dim=-1)
+    if min_p > 0.0:
+        p = torch.where(p < min_p * p.amax(dim=-1, keepdim=True), 0.0, p)
+        p /= p.sum(dim=-1, keepdim=True)
+    return p
+
+
+def serving_rounds(wl: Workload, rounds: int, bandit: str, device=0, seed: int = 0, min_p: float = 0.02, page: int = 16, longest: int = 400,
+                   pool_blocks: Optional[int] = None):
+    """The serving loop of Algorithm 1 around the library: per round the drafters are selected, the drafters' and the target's caches are
+    planned, the round is verified from cut probabilities and given random numbers (the drafters' rows in the order in which the
+    drafters hold them), and what was rejected or finished is given back.  Yields a dict per round; its tensors are the
+    loop's own and change with the next one.
+
+    Of a sequence with `length` tokens the target's cache holds all but the last.  A drafter that is chosen brings its own cache up to
+    date and adds its drafts but the last; of these the accepted ones stay.  A query ends at `longest` tokens: its bandit starts anew
+    and a prompt of another length takes its place."""
+    dev, i32 = torch.device("cuda", device), torch.int32
+    B, N, k = wl.B, wl.N, wl.k
+    T = wl.temperature if wl.temperature > 0 else 1.0
+    gen = RoundGenerator(wl, device=dev, seed=seed)
+    g = torch.Generator(device=dev).manual_seed(seed + 1)
+    most = (longest + 2 * k) // page + 1
+    blocks = B * most if pool_blocks is None else pool_blocks
+    msd = M.MetaSD(B, N, k, wl.V, dtype=wl.dtype, bandit=bandit, beta=wl.beta, gamma=wl.gamma, window=wl.tau, device=device)
+    drafters = M.BlockCache.empty(N, B, most, blocks, page, device)
+    target = M.BlockCache.empty(1, B, most, blocks, page, device)
+
+    def prompts():
+        return torch.randint(8, longest // 2, (B,), generator=g, device=dev).to(i32)
+
+    length, at = prompts(), torch.arange(B, device=dev)
+    in_target, in_drafters = torch.zeros(B, dtype=i32, device=dev), torch.zeros((N, B), dtype=i32, device=dev)
+    room = B * (longest + 2 * k)
+    try:
+        for t in range(rounds):
+            arm = msd.select()
+            played = arm.long()
+            goal_d, goal_t = length + (k - 1), length + k
+            plan_d = drafters.plan(goal_d, in_drafters, pool=arm, max_tokens=room)
+            plan_t = target.plan(goal_t, in_target, max_tokens=room)
+            rd = gen.gathered_round(t, arm.cpu().numpy())
+            p, q = cut_probabilities(rd["target"], T, min_p), cut_probabilities(rd["draft"], T, min_p)
+            tokens = torch.multinomial(q.reshape(B * k, wl.V), 1, generator=g).reshape(B, k).to(i32)
+            held = torch.empty_like(q)
+            held[plan_d.place.long()] = q
+            u, v = torch.rand((B, k), generator=g, device=dev), torch.rand(B, generator=g, device=dev)
+            res = msd.verify_probs(p, held, tokens, u, v, seed=seed, draft_place=plan_d.place, want_d_tv=True)
+            yield dict(t=t, arm=arm, length=length, in_drafters=in_drafters, in_target=in_target, goal_d=goal_d, goal_t=goal_t, plan_d=plan_d,
+                       plan_t=plan_t, target=p, draft=q, tokens=tokens, u_accept=u, u_draw=v, result=res, msd=msd, drafters=drafters,
+                       target_cache=target, best_arm=gen.best_arm(t))
+            in_target = length + res.accepted_len
+            in_drafters = in_drafters.clone()
+            in_drafters[played, at] = torch.maximum(in_drafters[played, at], torch.minimum(goal_d, in_target))
+            length = in_target + 1
+            done = length >= longest
+            length = torch.where(done, prompts(), length)
+            in_target = torch.where(done, 0, in_target)
+            in_drafters = torch.where(done, 0, in_drafters)
+            target.release(in_target)
+            drafters.release(in_drafters)
+            msd.reset(torch.where(done, at, -1).to(i32))      # ids outside the batch are passed over
+    finally:
+        msd.close()
+
+
+def serving_run(wl: Workload, rounds: int, bandit: str, **options) -> dict:
+    """serving_rounds, summed up: entries that the drafters' and the target's caches add per sequence and round (k - 1 drafts
+    and k + 1 tokens if nobody fell behind and all was accepted), the share of rounds in which a drafter had to catch up with more than
+    the last round, blocks held per sequence, the best-arm ratio and the block efficiency."""
+    entries_d = entries_t = behind = held = acc = best = 0.0
+    status = 0
+    for r in serving_rounds(wl, rounds, bandit, **options):
+        played = r["in_drafters"][r["arm"].long(), torch.arange(wl.B, device=r["arm"].device)]
+        behind += float((r["length"] - played > wl.k + 1).float().mean())
+        entries_d += float(r["plan_d"].token_start[-1]) / wl.B
+        entries_t += float(r["plan_t"].token_start[-1]) / wl.B
+        held += float(r["drafters"].held.sum() + r["target_cache"].held.sum()) / wl.B
+        acc += float(r["result"].accepted_len.float().mean())
+        best += float((r["arm"].cpu().numpy() == r["best_arm"]).mean())
+        status |= r["msd"].last_status() | r["drafters"].last_status() | r["target_cache"].last_status()
+    return dict(workload=wl.name, bandit=bandit, rounds=rounds, drafter_entries=entries_d / rounds, target_entries=entries_t / rounds,
+                behind_ratio=behind / rounds, blocks_held=held / rounds, best_arm_ratio=best / rounds,
+                block_efficiency=1.0 + acc / rounds, status=status)
+
+
 def constant_alignment_rows(B: int, k: int, V: int, alphas, dtype=torch.float32, device="cuda", seed: int = 0):
     """Rows with a prescribed alignment 1 - d_TV(p_j, q_j) = alphas[b, j]: the drafter puts all its mass on one
     token x (which is therefore the drafted token), the target gives x the probability alpha and a second token the
@@ -179,6 +269,7 @@ def main():
     ap.add_argument("--bandits", default="ucb,ducb")
     ap.add_argument("--window", type=int, default=25)
     ap.add_argument("--drafter-rounds", type=int, default=10, help="rounds per drafter of the reward-statistics table")
+    ap.add_argument("--serve", type=int, default=0, help="rounds of the serving loop with paged caches, per bandit")
     args = ap.parse_args()
     wl = WORKLOADS[args.workload]
     if args.batch:
@@ -187,11 +278,16 @@ def main():
     report["drafters"] = drafter_reward_statistics(wl, args.drafter_rounds)
     report["runs"] = [bandit_run(wl, args.rounds, reward, bandit, window=args.window)
                       for bandit in args.bandits.split(",") for reward in (M.REWARD_BD, M.REWARD_BE)]
+    if args.serve:
+        report["serving"] = [serving_run(wl, args.serve, bandit) for bandit in args.bandits.split(",")]
     print(json.dumps(report))
     print(format_table(report["drafters"], ["sigma", "samples", "mean_bd", "var_bd", "mean_be", "var_be", "be_zero_ratio",
                                             "block_efficiency", "signal_bd", "signal_be"]))
     print(format_table(report["runs"], ["bandit", "reward", "best_arm_ratio", "mean_bd", "var_bd", "mean_be", "var_be",
                                         "be_zero_ratio", "block_efficiency"]))
+    if args.serve:
+        print(format_table(report["serving"], ["bandit", "drafter_entries", "target_entries", "behind_ratio", "blocks_held", "best_arm_ratio",
+                                               "block_efficiency"]))
     for r in report["runs"]:
         print("%s/%s best-arm ratio per %d rounds: %s" % (r["bandit"], r["reward"], r["window"],
                                                          " ".join("%.2f" % v for v in r["best_arm_ratio_by_window"])))
