@@ -300,7 +300,8 @@ int metasd_verify_noalloc(int32_t batch, int32_t k, int32_t vocab, int32_t logit
  *                        the first rejection n (w = p_n where that leaves nothing), w = p at position k_b if all were accepted
  *   d_tv[b, j]           1/2 sum_v |p_j(v) - q_j(v)|, j < k_b
  *
- * The rows need not be normalised: the accept test takes the values as they are, the draw divides by its own sum.  Without d_tv
+ * The rows need not be normalised: the accept test takes the values as they are, the draw divides by its own sum (sums of a row stay
+ * within the range of fp32; beyond it they count as not finite).  Without d_tv
  * only the drafted tokens' entries and the row (pair) that the next token is drawn from are read.
  *
  *   ctx            NULL: stateless.  Else the round is one of this context's: batch <= max_batch, 1 <= k <= max_draft, vocab as
@@ -324,6 +325,7 @@ int metasd_verify_noalloc(int32_t batch, int32_t k, int32_t vocab, int32_t logit
  *   reward         with a context: [batch] fp32; else NULL
  *   status         optional, without a context: device uint32 that METASD_STATUS_* bits are OR-ed into
  *
+ * Uniforms outside [0, 1) do no harm: NaN rejects, and draws the last token with weight, as 1 and above do; below 0 the first.
  * Defined outcomes: an entry of a drafted token that is NaN, infinite or negative rejects it, a row that holds such an entry has
  * d_TV 1 and gives token -1, as a row of zeros does (METASD_STATUS_NONFINITE); a drafted token outside the vocabulary is
  * rejected; a certain drafter's distance to such a token is 1; q(x) = 0 < p(x) is accepted.

@@ -14,7 +14,8 @@ class Caches:
         pool = [0] * batch if pool is None else [int(g) for g in pool]
         part = [g if 0 <= g < self.pools else self.pools for g in pool]
         order = [b for g in range(self.pools + 1) for b in range(batch) if part[b] == g]
-        place = [order.index(b) for b in range(batch)]
+        where = {b: i for i, b in enumerate(order)}
+        place = [where[b] for b in range(batch)]
         pool_start = [sum(p < g for p in part) for g in range(self.pools + 1)]
         token_start, entries, short = [0], [], set()
         for b in order:

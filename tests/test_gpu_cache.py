@@ -88,6 +88,50 @@ def test_long_and_uneven_prompts(lengths):
     assert cache.free_count.tolist() == [6000]
 
 
+@pytest.mark.parametrize("batch,pools", [(9000, 3), (65535, 1), (20000, 16)])
+def test_very_many_sequences(batch, pools):
+    """More sequences than a block has threads, and than its shared memory has places."""
+    rng = np.random.default_rng(batch)
+    page, most = 4, 5
+    cache, ref = pair(pools, batch, most, batch * 3, page, seed=batch)
+    cached = np.zeros((pools, batch), dtype=np.int64)
+    pool = rng.integers(-1, pools, size=batch)
+    goal = np.where(rng.random(batch) < 0.3, rng.integers(0, most * page + 1, size=batch), 0)
+    plan_both(cache, ref, goal, cached, pool if pools > 1 else None)
+    keep = np.minimum(rng.integers(0, most * page, size=(pools, batch)), goal)
+    cache.release(ints(keep))
+    ref.release(keep)
+    same(cache, ref)
+    have = np.zeros((pools, batch), dtype=np.int64)
+    at = np.maximum(pool, 0), np.arange(batch)
+    have[at] = np.where(pool >= 0, keep[at], 0) if pools > 1 else keep[0]
+    plan_both(cache, ref, goal, have, pool if pools > 1 else None)
+
+
+def test_tables_beyond_32_bits():
+    """Block tables with more than 2^31 entries in all, and more blocks in a step than 2^31 if everyone took all."""
+    batch, most = 60000, 18000
+    cache = M.BlockCache.empty(2, batch, most, 200000, 16)
+    assert cache.block_table.numel() > 2 ** 31
+    lengths = np.zeros(batch, dtype=np.int64)
+    lengths[[0, 777, 40000, batch - 1]] = [5, 16 * 300, 16 * most, 33]
+    pool = np.ones(batch, dtype=np.int64)
+    out = cache.plan(ints(lengths), ints(np.zeros(batch)), pool=ints(pool), max_tokens=400000)
+    assert cache.last_status() == 0
+    need = -(-lengths // 16)
+    first = 0
+    for b in np.flatnonzero(lengths):
+        ids = np.arange(first, first + need[b])      # the pool hands out 0, 1, 2, ..
+        assert np.array_equal(cache.block_table[1, b, :need[b]].cpu().numpy(), ids)
+        start = int(out.token_start[int(out.place[b])])
+        assert np.array_equal(out.slot_map[start:start + lengths[b]].cpu().numpy(), first * 16 + np.arange(lengths[b]))
+        first += need[b]
+    assert int(cache.held[1].sum()) == first and int(cache.free_count[1]) == 200000 - first
+    cache.release(ints(np.zeros(batch)))
+    assert cache.last_status() == 0 and cache.free_count.tolist() == [200000, 200000]
+    assert torch.equal(cache.free_blocks[0], cache.free_blocks[1]) and int(cache.held.sum()) == 0
+
+
 def test_a_release_undoes_a_plan():
     cache, ref = pair(4, 50, 30, 800, 8, seed=3)
     rng = np.random.default_rng(3)

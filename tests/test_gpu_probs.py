@@ -246,6 +246,89 @@ def test_mass_at_every_place_is_found():
             assert out.next_token.tolist() == spots
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_parts_of_several_batches(dtype):
+    """Vocabularies of which a part is read in several steps, and looked through in several."""
+    V = 1200003
+    check(inputs(2, 1, V, dtype, seed=70, cut=0.01), status=None)
+    spots = [0, 511, 512, 5119, 5120, 5121, 10239, 10240, 20480, 600000, 1199999, 1200000, 1200002]
+    p = torch.zeros((len(spots), 1, V), dtype=DTYPES[dtype], device=DEV)
+    p[torch.arange(len(spots)), 0, torch.tensor(spots)] = 0.3
+    out = M.verify_probs(p, None, None, None, torch.full((len(spots),), 0.7, device=DEV))
+    assert out.next_token.tolist() == spots
+
+
+def test_rows_beyond_32_bit_offsets():
+    V, k = 4099, 2
+    s = inputs(2, k, V, "bf16", seed=71)
+    far = 2 ** 31 + 77
+    def apart(t):
+        wide = torch.zeros(far + t.shape[1] * V + 16, dtype=t.dtype, device=DEV)
+        view = wide.as_strided((2, t.shape[1], V), (far, V, 1))
+        view.copy_(t)
+        return view
+    check(dict(s, target=apart(s["target"]), draft=apart(s["draft"])), status=None)
+
+
+def test_the_smallest_numbers():
+    """Rows of subnormal numbers: what is left over of them is drawn from all the same."""
+    V = 600
+    s = inputs(6, 2, V, "fp32", seed=72)
+    s["target"].mul_(2.0 ** -130)
+    s["draft"].mul_(2.0 ** -130)
+    assert float(s["target"].max()) < 2.0 ** -126
+    ref = R.verify(host(s["target"]), host(s["draft"]), s["tokens"].cpu().numpy(), host(s["u_accept"]), host(s["u_draw"]))
+    out = M.verify_probs(s["target"], s["draft"], s["tokens"], s["u_accept"], s["u_draw"])
+    assert ref[3] == 0 and (ref[1] >= 0).all()
+    assert np.array_equal(out.accepted_len.cpu().numpy(), ref[0]) and np.array_equal(out.next_token.cpu().numpy(), ref[1])
+
+
+def test_calls_on_two_streams_at_once():
+    """Stateless calls share nothing: two streams that run side by side give what each gives alone."""
+    s = [inputs(64, 4, 32000, dtype, seed=80 + i) for i, dtype in enumerate(("fp32", "bf16"))]
+    call = lambda x: M.verify_probs(x["target"], x["draft"], x["tokens"], x["u_accept"], x["u_draw"], want_d_tv=True)
+    want = [call(x) for x in s]
+    streams = [torch.cuda.Stream() for _ in s]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(8):
+        for i, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                got[i].append(call(s[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for out in got[i]:
+            for name in ("accepted_len", "next_token", "d_tv"):
+                assert torch.equal(getattr(out, name), getattr(want[i], name))
+
+
+def test_a_contexts_round_captured_and_replayed():
+    """Every replay is the context's next round."""
+    B, K, k, V = 10, 4, 3, 2003
+    ctx = [M.MetaSD(B, K, k, V, dtype="bf16", bandit="ducb") for _ in range(2)]
+    s = inputs(B, k, V, "bf16", seed=90)
+    args = (s["target"], s["draft"], s["tokens"], s["u_accept"], s["u_draw"])
+    out, arm = ctx[0].verify_probs(*args), ctx[0].select()
+    ctx[0].reset()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        ctx[0].verify_probs(*args, out=out)
+        ctx[0].select(out=arm)
+    for t in range(7):
+        more = inputs(B, k, V, "bf16", seed=91 + t)
+        for name in s:
+            s[name].copy_(more[name])
+        graph.replay()
+        want = ctx[1].verify_probs(*args)
+        assert torch.equal(arm, ctx[1].select())
+        for name in ("accepted_len", "next_token", "reward"):
+            assert torch.equal(getattr(out, name), getattr(want, name))
+    assert ctx[0].state_export() == ctx[1].state_export()
+    for c in ctx:
+        c.close()
+
+
 @pytest.mark.parametrize("V,dtype", [(50257, "fp32"), (32000, "bf16")])
 def test_results_do_not_depend_on_the_batch(V, dtype):
     """Alone, in a few and in many: the launch's shape changes, no bit of the results does."""
