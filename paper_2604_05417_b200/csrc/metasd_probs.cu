@@ -339,16 +339,16 @@ __device__ __forceinline__ int find_token(const PairOfRows<LT> &r, bool pair, Cr
         float p[VEC], q[VEC];
         Logit<LT>::unpack(ra, p);
         Logit<LT>::unpack(rd, q);
-        double w[VEC], mine = 0.0;
+        Sums x = {0ull, 0ull, 0ull, false};
         int last = -1;
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
             if (!pair) q[e] = g * VEC + e == r.certain ? 1.f : 0.f;
-            w[e] = p[e] > q[e] ? (double)p[e] - (double)q[e] : 0.0;
-            if (w[e] > 0.0) last = g * VEC + e;
+            if (p[e] > q[e]) last = g * VEC + e;
         }
 #pragma unroll
-        for (int e = 0; e < VEC; e += 2) mine += w[e] + w[e + 1];
+        for (int e = 0; e < VEC; e += 2) add_pair<true, false>(x, pack2(p[e], p[e + 1]), pack2(q[e], q[e + 1]));
+        const double mine = weight_of(x);
         const double upto = lanes_up_to(mine);
         double start = __shfl_up_sync(FULL, upto, 1);
         if (lane == 0) start = 0.0;
@@ -367,8 +367,9 @@ __device__ __forceinline__ int find_token(const PairOfRows<LT> &r, bool pair, Cr
             bool done = false;
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
-                run += w[e];
-                if (!done && w[e] > 0.0) {
+                const bool some = p[e] > q[e];
+                run += some ? (double)p[e] - (double)q[e] : 0.0;
+                if (!done && some) {
                     token = g * VEC + e;
                     done = run > threshold;
                 }
@@ -440,20 +441,23 @@ __global__ void __launch_bounds__(THREADS, 4) probs_kernel(const ProbsParams p)
     r.V = V;
     r.n_vec = (V + VEC - 1) / VEC;
     r.certain = -1;
+    const float u_draw = rank == 0 && warp == 0 ? __ldg(p.u_draw + b) : 0.f;
+    // The accept tests, a lane each, by one warp.
+    int x = -1;
+    float u = 0.f;
+    if (warp == 0 && lane < kb) {
+        x = __ldg(tokens + lane);
+        u = __ldg(p.u_accept + (int64_t)b * k + lane);
+    }
     if (TV && j < kb) {     // this row is read whatever the tests say: its first lines come meanwhile
         rows_of(j);
         if (!draft) r.certain = __ldg(tokens + j);
         if (s0 < s1) prefetch_batch(r, pair, s0 * part_vecs);
     }
-    const float u_draw = rank == 0 && warp == 0 ? __ldg(p.u_draw + b) : 0.f;
-    // The accept tests, a lane each, by one warp.
     if (warp == 0) {
         bool accepted = false;
         uint32_t f = 0;
-        int x = -1;
         if (lane < kb) {
-            x = __ldg(tokens + lane);
-            const float u = __ldg(p.u_accept + (int64_t)b * k + lane);
             if (x < 0 || x >= V) {
                 f |= METASD_STATUS_TOKEN_OOR;
             } else {
