@@ -75,33 +75,27 @@ template <typename LT, bool SHIFTED> __device__ __forceinline__ uint4 vector_at(
     return n < VEC ? cut<LT>(v, n) : v;
 }
 
-// Whether any entry of the vectors may be no probability (NaN, infinite, or with its sign set): the largest bit pattern.
-template <typename LT> __device__ __forceinline__ bool suspicious(const uint4 &v)
-{
-    if constexpr (sizeof(LT) == 2) {
-        const uint32_t m = __vmaxu2(__vmaxu2(v.x, v.y), __vmaxu2(v.z, v.w));
-        return m >= 0x7F800000u || (m & 0xFFFFu) >= 0x7F80u;
-    } else {
-        return max(max(v.x, v.y), max(v.z, v.w)) >= 0x7F800000u;
-    }
-}
 __device__ __forceinline__ bool is_probability(float x) { return x >= 0.f && x < INFINITY; }   // -0 is one
 
-// Sums of a lane, as packed pairs.
+// Sums of a lane.  NaN and infinite entries make those they come into NaN; what has its sign set is looked for apart.
 struct Sums {
-    uint64_t over;      // of max(0, p - q), the differences as rounded, rounded again at every addition
-    uint64_t rest;      // what these roundings left out
-    uint64_t under;     // of max(0, q - p)
-    bool bad;
+    uint64_t over;          // of max(0, p - q), the differences as rounded, rounded again at every addition; a packed pair
+    uint64_t rest;          // what these roundings left out
+    float apart, apart1;    // of |p - q|
+    bool bad;               // an entry below zero
+    __device__ __forceinline__ Sums() : over(0ull), rest(0ull), apart(0.f), apart1(0.f), bad(false) {}
 };
 
 __device__ __forceinline__ uint64_t sub2(uint64_t a, uint64_t b) { return fma2(b, pack2(-1.f), a); }
+// The larger of both, half by half; NaN where either is.
 __device__ __forceinline__ uint64_t max2(uint64_t a, uint64_t b)
 {
     float al, ah, bl, bh;
     unpack2(a, al, ah);
     unpack2(b, bl, bh);
-    return pack2(fmaxf(al, bl), fmaxf(ah, bh));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(al) : "f"(bl));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(ah) : "f"(bh));
+    return pack2(al, ah);
 }
 // sum += x, and what the rounding takes away goes to rest (x and the sum in any order of size).
 __device__ __forceinline__ void add_exactly(uint64_t &sum, uint64_t &rest, uint64_t x)
@@ -117,45 +111,56 @@ template <typename LT> __device__ __forceinline__ uint64_t pair_at(const uint4 &
     else return pack2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
 }
 
-// A pair of entries of both rows.  With m = max(p, q), m - q is max(0, p - q) with no comparison of its own.  `over` goes through
-// the same roundings whether what they take away is kept (EXACT: the row may be drawn from) or not.
-template <bool EXACT, bool TV> __device__ __forceinline__ void add_pair(Sums &s, uint64_t p, uint64_t q)
+// A pair of entries of both rows.  With m = max(p, q), m - q is max(0, p - q) with no comparison of its own.  WEIGHT: the row may be drawn
+// from; TV: its distance is wanted.  Neither changes the other.
+template <bool WEIGHT, bool TV> __device__ __forceinline__ void add_pair(Sums &s, uint64_t p, uint64_t q)
 {
-    const uint64_t m = max2(p, q), d = sub2(m, q);
-    if (EXACT) {
+    if (WEIGHT) {
+        const uint64_t m = max2(p, q), d = sub2(m, q);
         s.rest = add2(s.rest, sub2(sub2(m, d), q));
         add_exactly(s.over, s.rest, d);
-    } else {
-        s.over = add2(s.over, d);
     }
-    if (TV) s.under = add2(s.under, sub2(m, p));
+    if (TV) {
+        float lo, hi;
+        unpack2(sub2(p, q), lo, hi);
+        s.apart += fabsf(lo);
+        s.apart1 += fabsf(hi);
+    }
 }
 
-template <typename LT, bool PAIR, bool EXACT, bool TV>
+template <typename LT, bool PAIR, bool WEIGHT, bool TV>
 __device__ __forceinline__ void add_vectors(Sums &s, const uint4 &ra, const uint4 &rd, int tok0, int certain)
 {
     constexpr int VEC = Logit<LT>::VEC;
-    if (suspicious<LT>(ra) || (PAIR && suspicious<LT>(rd))) {
+    uint32_t signs = ra.x | ra.y | ra.z | ra.w;
+    if (PAIR) signs |= rd.x | rd.y | rd.z | rd.w;
+    if (signs & (sizeof(LT) == 2 ? 0x80008000u : 0x80000000u)) {
         float p[VEC], q[VEC];
         Logit<LT>::unpack(ra, p);
         Logit<LT>::unpack(rd, q);
 #pragma unroll
         for (int e = 0; e < VEC; ++e)
-            if (!is_probability(p[e]) || (PAIR && !is_probability(q[e]))) s.bad = true;
+            if (p[e] < 0.f || (PAIR && q[e] < 0.f)) s.bad = true;
     }
     if (PAIR) {
 #pragma unroll
-        for (int i = 0; i < VEC / 2; ++i) add_pair<EXACT, TV>(s, pair_at<LT>(ra, i), pair_at<LT>(rd, i));
+        for (int i = 0; i < VEC / 2; ++i) add_pair<WEIGHT, TV>(s, pair_at<LT>(ra, i), pair_at<LT>(rd, i));
     } else if (certain < tok0 || certain >= tok0 + VEC) {
 #pragma unroll
         for (int i = 0; i < VEC / 2; ++i) {
-            if (EXACT) add_exactly(s.over, s.rest, pair_at<LT>(ra, i));
-            else s.over = add2(s.over, pair_at<LT>(ra, i));
+            const uint64_t p = pair_at<LT>(ra, i);
+            if (WEIGHT) add_exactly(s.over, s.rest, p);
+            if (TV) {
+                float lo, hi;
+                unpack2(p, lo, hi);
+                s.apart += lo;
+                s.apart1 += hi;
+            }
         }
     } else {
 #pragma unroll
         for (int i = 0; i < VEC / 2; ++i)
-            add_pair<EXACT, TV>(s, pair_at<LT>(ra, i), pack2(certain == tok0 + 2 * i ? 1.f : 0.f, certain == tok0 + 2 * i + 1 ? 1.f : 0.f));
+            add_pair<WEIGHT, TV>(s, pair_at<LT>(ra, i), pack2(certain == tok0 + 2 * i ? 1.f : 0.f, certain == tok0 + 2 * i + 1 ? 1.f : 0.f));
     }
 }
 
@@ -217,28 +222,28 @@ template <typename LT, bool SHIFTED> __device__ __forceinline__ uint4 load_behin
     return SHIFTED && lead ? ld_stream(row + c + 32 * BATCH) : make_uint4(0u, 0u, 0u, 0u);
 }
 
-template <typename LT, bool PAIR, bool EXACT, bool TV>
+template <typename LT, bool PAIR, bool WEIGHT, bool TV>
 __device__ __forceinline__ void add_batch(Sums &s, const uint4 (&ra)[BATCH], const uint4 (&rd)[BATCH], int c, int certain)
 {
     constexpr int VEC = Logit<LT>::VEC;
 #pragma unroll
-    for (int i = 0; i < BATCH; ++i) add_vectors<LT, PAIR, EXACT, TV>(s, ra[i], rd[i], (c + 32 * i + (int)(threadIdx.x & 31)) * VEC, certain);
+    for (int i = 0; i < BATCH; ++i) add_vectors<LT, PAIR, WEIGHT, TV>(s, ra[i], rd[i], (c + 32 * i + (int)(threadIdx.x & 31)) * VEC, certain);
 }
 
 // A warp's sums of a part, put where the sequence's sums are collected.
-template <bool EXACT, bool TV> __device__ __forceinline__ void publish(const Sums &x, int s, uint32_t weights_at, uint32_t apart_at)
+template <bool WEIGHT, bool TV> __device__ __forceinline__ void publish(const Sums &x, int s, uint32_t weights_at, uint32_t apart_at)
 {
-    const double w = EXACT ? warp_sum(weight_of(x)) : 0.0;
-    const float apart = TV ? warp_sum_f(sum2(add2(x.over, x.under))) : 0.f;
+    const double w = WEIGHT ? warp_sum(weight_of(x)) : 0.0;
+    const float apart = TV ? warp_sum_f(x.apart + x.apart1) : 0.f;
     const bool bad = __any_sync(FULL, x.bad);
     if ((threadIdx.x & 31) == 0) {
         st_cluster(weights_at + 8u * s, bad ? (double)NAN : w);
-        if (TV) st_cluster(apart_at + 4u * s, __float_as_int(apart));
+        if (TV) st_cluster(apart_at + 4u * s, __float_as_int(bad ? NAN : apart));
     }
 }
 
 // The parts s0, s0 + step, .. below s1 of a row (pair), by one warp.  The order of additions does not depend on where the rows
-// start, and keeping what the roundings take away (EXACT) does not change the other sums.
+// start, and the sums that a draw needs (WEIGHT) do not change those of the distance.
 // Asks L2 for a batch: 2 KB of each row, a line per lane.
 template <typename LT> __device__ __forceinline__ void prefetch_batch(const PairOfRows<LT> &r, bool pair, int c)
 {
@@ -247,14 +252,14 @@ template <typename LT> __device__ __forceinline__ void prefetch_batch(const Pair
     if ((lane < 16 || pair) && g < r.n_vec) asm volatile("prefetch.global.L2 [%0];" ::"l"(row + g));
 }
 
-template <typename LT, bool PAIR, bool EXACT, bool TV, bool SHIFTED>
+template <typename LT, bool PAIR, bool WEIGHT, bool TV, bool SHIFTED>
 __device__ __forceinline__ void sum_parts(const PairOfRows<LT> r, int part_vecs, int s0, int s1, int step, uint32_t weights_at, uint32_t apart_at)
 {
     constexpr int VEC = Logit<LT>::VEC;
     const int whole = r.V / VEC;
     for (int s = s0; s < s1; s += step) {
         const int g0 = s * part_vecs, g1 = min(g0 + part_vecs, r.n_vec);
-        Sums x = {0ull, 0ull, 0ull, false};
+        Sums x;
         int c = g0;
         // whole vectors, whole batches: nothing but loads and sums
         for (; c + 32 * BATCH <= min(g1, whole); c += 32 * BATCH) {
@@ -267,28 +272,28 @@ __device__ __forceinline__ void sum_parts(const PairOfRows<LT> r, int part_vecs,
                 if (SHIFTED) realign<LT>(rd, behind_d, r.lead_d);
             }
             if (SHIFTED) realign<LT>(ra, behind_a, r.lead_a);
-            add_batch<LT, PAIR, EXACT, TV>(x, ra, PAIR ? rd : ra, c, r.certain);
+            add_batch<LT, PAIR, WEIGHT, TV>(x, ra, PAIR ? rd : ra, c, r.certain);
         }
         // the row's end
 #pragma unroll 1
         for (int g = c + (threadIdx.x & 31); g < g1; g += 32) {
             const uint4 ra = vector_at<LT, SHIFTED>(r.a, r.lead_a, g, r.V);
             const uint4 rd = PAIR ? vector_at<LT, SHIFTED>(r.d, r.lead_d, g, r.V) : ra;
-            add_vectors<LT, PAIR, EXACT, TV>(x, ra, rd, g * VEC, r.certain);
+            add_vectors<LT, PAIR, WEIGHT, TV>(x, ra, rd, g * VEC, r.certain);
         }
-        publish<EXACT, TV>(x, s, weights_at, apart_at);
+        publish<WEIGHT, TV>(x, s, weights_at, apart_at);
     }
 }
 
-template <typename LT, bool EXACT, bool TV>
+template <typename LT, bool WEIGHT, bool TV>
 __device__ __forceinline__ void sum_parts(const PairOfRows<LT> &r, bool pair, int part_vecs, int s0, int s1, int step, uint32_t weights_at, uint32_t apart_at)
 {
     if (pair) {
-        if ((r.lead_a | r.lead_d) == 0) sum_parts<LT, true, EXACT, TV, false>(r, part_vecs, s0, s1, step, weights_at, apart_at);
-        else sum_parts<LT, true, EXACT, TV, true>(r, part_vecs, s0, s1, step, weights_at, apart_at);
+        if ((r.lead_a | r.lead_d) == 0) sum_parts<LT, true, WEIGHT, TV, false>(r, part_vecs, s0, s1, step, weights_at, apart_at);
+        else sum_parts<LT, true, WEIGHT, TV, true>(r, part_vecs, s0, s1, step, weights_at, apart_at);
     } else {
-        if (r.lead_a == 0) sum_parts<LT, false, EXACT, TV, false>(r, part_vecs, s0, s1, step, weights_at, apart_at);
-        else sum_parts<LT, false, EXACT, TV, true>(r, part_vecs, s0, s1, step, weights_at, apart_at);
+        if (r.lead_a == 0) sum_parts<LT, false, WEIGHT, TV, false>(r, part_vecs, s0, s1, step, weights_at, apart_at);
+        else sum_parts<LT, false, WEIGHT, TV, true>(r, part_vecs, s0, s1, step, weights_at, apart_at);
     }
 }
 
@@ -339,7 +344,7 @@ __device__ __forceinline__ int find_token(const PairOfRows<LT> &r, bool pair, Cr
         float p[VEC], q[VEC];
         Logit<LT>::unpack(ra, p);
         Logit<LT>::unpack(rd, q);
-        Sums x = {0ull, 0ull, 0ull, false};
+        Sums x;
         int last = -1;
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
@@ -507,7 +512,6 @@ __global__ void __launch_bounds__(THREADS, 4) probs_kernel(const ProbsParams p)
             for (int i = 0; i < PER; ++i) mine += w[i];
             const double upto = lanes_up_to(mine), total = __shfl_sync(FULL, upto, 31);
             const bool bad = !(total < INFINITY);
-            if (bad) flags |= METASD_STATUS_NONFINITE;
             Crossing x = {0.0, 0.0, 0, 0, -1, false};      // nothing to look for
             if (n == j) {       // the row that the token is drawn from
                 if (total > 0.0 && !bad) {
@@ -546,7 +550,9 @@ __global__ void __launch_bounds__(THREADS, 4) probs_kernel(const ProbsParams p)
                 apart = warp_sum(apart);
                 // a token outside the vocabulary has no place in the row
                 const bool nowhere = !pair && (r.certain < 0 || r.certain >= V);
-                if (lane == 0) p.d_tv[(int64_t)b * k + j] = bad || nowhere ? 1.f : (float)(0.5 * apart);
+                const bool finite = apart < INFINITY;
+                if (!finite) flags |= METASD_STATUS_NONFINITE;
+                if (lane == 0) p.d_tv[(int64_t)b * k + j] = !finite || nowhere ? 1.f : (float)(0.5 * apart);
             }
             if (lane == 0) {
                 if (n == j && !x.again) p.accepted_len[b] = n;
