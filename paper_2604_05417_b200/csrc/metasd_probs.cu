@@ -597,11 +597,23 @@ cudaError_t launch_probs(const ProbsParams &params, int dtype, int n_sm, cudaStr
     p.part_vecs = (int)(step * std::max(1ll, (n_vec + step * MAX_PARTS - 1) / (step * MAX_PARTS)));
     p.parts = (int)((n_vec + p.part_vecs - 1) / p.part_vecs);
     const long long jobs = (long long)p.batch * (p.d_tv ? p.k + 1 : 1);
-    // rows that are read: with distances the bonus row of a few sequences only, and of ragged drafts about half
-    const long long rows = p.d_tv ? (long long)p.batch * (p.draft_len ? (p.k + 1) / 2 : p.k) : p.batch;
-    // As many blocks of a cluster as leave all rows in flight at once (four blocks fit an SM) and every warp a part.
+    // Blocks that share a row.  `rows`: those that are read (with distances the bonus row of a few sequences only; of ragged drafts about half of
+    // the slots, whose other blocks end at once).  More blocks a row shorten a launch's last wave of four blocks an SM, and cost a
+    // start, a meeting and a smaller stretch each.  Us with 1, 2, 4 and 8 (fp32 rows without distances unless it says so):
+    //   V = 128256, rows 100: 53.7, 32.7, 22.4, 24.1; 300: 65.0, 58.8, 51.5, 53.8; 600: 108.0, 91.9, 91.1, 99.9; 900: 141.1, 125.9, 131.4, 145.4
+    //   V = 152064, rows 440: 78.0, 84.5, 77.6; 512: 84.8, 90.3, 89.3; 620: 122.5, 105.6, 104.9
+    //   V = 128256, bf16 with distances, rows 40: 28.9, 18.5, 13.1, 11.0; 448: 55.4, 48.0, 46.0, 52.4; 1190: 113.5, 103.0, 107.5, 128.1;
+    //     1792: 154.0, 152.9, 168.0
+    //   V = 50264 with distances, rows 120: 26.8, 18.3, 14.7, 15.8; 300: 32.7, 31.7, 28.7, 32.7; 640: 57.4, 49.0, 50.3, 65.3
+    //   V = 32000, bf16, rows 100: 9.4, 8.9, 8.1, 10.1; 300: 16.2, 13.9, 15.6, 23.6; 600: 21.8, 23.8, 28.7; 1000: 30.7, 35.7, 44.6
+    const double rows = !p.d_tv ? p.batch : p.draft_len ? 0.55 * p.batch * (p.k + 1) : (double)p.batch * p.k;
+    const auto waves = [&](int blocks) { return rows * blocks / (4.0 * n_sm); };
+    const bool lengthy = n_vec >= 8192;     // 128 KB
     int cluster = 1;
-    while (cluster < 8 && 2 * rows * cluster <= 4 * n_sm && p.parts > WARPS * cluster) cluster *= 2;
+    while (cluster <= 8 && !(waves(cluster) >= 0.75 && waves(cluster) <= 1.0)) cluster *= 2;      // one wave, well filled
+    if (cluster > 8)
+        cluster = waves(8) <= 1.0 ? 8 : waves(4) <= (lengthy ? n_vec >= 24576 ? 2.75 : 2.1 : 1.0) ? 4 : waves(2) <= (lengthy ? 8.0 : 1.35) ? 2 : 1;
+    while (cluster > 1 && p.parts <= WARPS * cluster / 2) cluster /= 2;
     auto launch = [&](auto kernel) { return launch_kernel(kernel, (unsigned)(jobs * cluster), THREADS, 0, cluster, true, stream, p); };
     if (dtype == METASD_BF16) return p.d_tv ? launch(probs_kernel<__nv_bfloat16, true>) : launch(probs_kernel<__nv_bfloat16, false>);
     return p.d_tv ? launch(probs_kernel<float, true>) : launch(probs_kernel<float, false>);
