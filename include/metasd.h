@@ -10,6 +10,8 @@
  *                    the alignment reward (Definition 2, Eq. 4; or block efficiency, Sec. 2.3),
  *                    the bandit update (Algorithm 2, statistics update; Discounted UCB and Sliding-window
  *                    UCB of the non-stationary appendix) and the next round's selection.
+ *   metasd_verify_probs : the same from probabilities and random numbers of the caller's.
+ *   metasd_cache_plan, metasd_cache_release : block tables and slot maps of the models' paged caches.
  *
  * Conventions
  *   - Every pointer is a DEVICE pointer unless the parameter name starts with host_.
@@ -34,7 +36,7 @@
  *   - Every function returns 0 (METASD_OK) or a negative metasd_error.  Device-side anomalies
  *     never trap: they set bits in the context's status word and produce the defined outputs
  *     described at metasd_last_status.
- *   - There is no CPU fallback: without a CUDA device metasd_init fails with METASD_ERR_CUDA.
+ *   - There is no CPU fallback: without a CUDA device metasd_init, and the calls without a context, fail with METASD_ERR_CUDA.
  */
 #ifndef METASD_H
 #define METASD_H
