@@ -369,7 +369,7 @@ size_t metasd_cache_workspace_bytes(int32_t max_batch, int32_t n_pools);   /* 0:
  *   order         optional [batch]: the sequences by pool, in sequence order within each; those that take no part at the end
  *   place         optional [batch]: the inverse, order[place[b]] == b
  *   pool_start    optional [n_pools + 1]: the first place of each pool, and the first of those that take no part
- *   token_start   [batch + 1], by place: running sum of the new entries
+ *   token_start   [batch + 1], by place: running sum of the new entries (it stops at 2^31 - 1, behind every max_tokens)
  *   slot_map      [max_tokens] int64: block_table[pool][b][position / page_size] * page_size + position % page_size of every
  *                 new entry; -1: its sequence is not planned (METASD_STATUS_NO_BLOCKS, METASD_STATUS_TRUNCATED)
  *   position      optional [max_tokens]; sequence: optional [max_tokens], the sequence of every new entry

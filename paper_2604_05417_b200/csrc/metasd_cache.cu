@@ -109,7 +109,7 @@ struct Place {
         held = e.held;
         planned = e.first != -1;
         table = p.c.block_table + ((int64_t)e.pool * p.c.max_batch + e.sequence) * p.c.max_blocks;
-        taken = p.c.free_blocks + (int64_t)e.pool * p.c.n_blocks + (e.held + e.first);
+        taken = p.c.free_blocks + (int64_t)e.pool * p.c.n_blocks + ((int64_t)e.held + e.first);
     }
     __device__ __forceinline__ int id(int block) const { return planned ? *(block >= held ? taken - block : table + block) : 0; }
     __device__ __forceinline__ void note(int block, int id) const
