@@ -196,6 +196,23 @@ __device__ __forceinline__ void fill(const CachePlanParams &p, const PlanEntry *
     }
 }
 
+// The same, an entry to a thread, where there are enough of them: a second entry of another sequence is a second chain of loads.
+template <int THREADS, typename Starts>
+__device__ __forceinline__ void fill_singly(const CachePlanParams &p, const PlanEntry *entries, const Starts &token_start, int begin, int end)
+{
+    for (int t = begin + (int)threadIdx.x; t < end; t += THREADS) {
+        const int at = place_of(token_start, 0, p.batch, t);
+        Place x;
+        x.at(p, entries[at]);
+        const int position = x.cached + (t - token_start[at]), block = divide(position, p.c.page_size, p.page_inverse);
+        const int in = position - block * p.c.page_size, id = x.id(block);
+        if (in == 0) x.note(block, id);
+        p.slot_map[t] = x.slot(p, id, in);
+        if (p.position) p.position[t] = position;
+        if (p.sequence) p.sequence[t] = x.sequence;
+    }
+}
+
 // Shared memory of the first kernel.
 template <int THREADS> struct PlanShared {
     int tally[KEYS][MOST_WARPS];        // sequences of a pool in front of a warp's, then the places behind them
@@ -460,12 +477,14 @@ template <int THREADS, bool FILLS> __global__ void __launch_bounds__(THREADS) pl
             __syncthreads();
         }
         const PlanEntry *entries = rank == 0 && p.narrow && batch <= THREADS ? sh.entries : (const PlanEntry *)p.c.workspace;
-        const int total = min(near ? sh.token_start[batch] : __ldcg(p.token_start + batch), p.max_tokens), share = 2 * THREADS;
-        for (long long begin = (long long)share * rank; begin < total; begin += (long long)share * ranks) {
-            const int end = (int)min(begin + share, (long long)total);
-            if (near) fill<THREADS>(p, entries, InShared{sh.token_start}, (int)begin, end);
-            else fill<THREADS>(p, entries, InGlobal{p.token_start}, (int)begin, end);
-        }
+        // a stretch each, of the entries that there are
+        const int total = min(near ? sh.token_start[batch] : __ldcg(p.token_start + batch), p.max_tokens);
+        const int each = (total / ranks / 32 + 1) * 32;
+        const long long begin = (long long)each * rank;
+        const int end = (int)min(begin + each, (long long)total);
+        if (begin >= total) return;
+        if (near) fill_singly<THREADS>(p, entries, InShared{sh.token_start}, (int)begin, end);
+        else fill_singly<THREADS>(p, entries, InGlobal{p.token_start}, (int)begin, end);
     }
 }
 
@@ -478,7 +497,8 @@ __global__ void __launch_bounds__(FILL_THREADS, FILL_BLOCKS) fill_kernel(const C
     const PlanEntry *entries = (const PlanEntry *)p.c.workspace;
     const bool near = p.batch <= STARTS;
     const int total = min(__ldcg(p.token_start + p.batch), p.max_tokens);
-    const long long turn = 2 * FILL_THREADS, turns = (total + turn - 1) / turn, each = (turns + gridDim.x - 1) / gridDim.x * turn;
+    const bool few = total <= (long long)gridDim.x * FILL_THREADS;      // an entry to a thread
+    const long long turn = few ? 32 : 2 * FILL_THREADS, turns = (total + turn - 1) / turn, each = (turns + gridDim.x - 1) / gridDim.x * turn;
     const long long begin = each * blockIdx.x;
     if (begin >= total) return;
     if (near) {
@@ -486,8 +506,12 @@ __global__ void __launch_bounds__(FILL_THREADS, FILL_BLOCKS) fill_kernel(const C
         __syncthreads();
     }
     const int end = (int)min(begin + each, (long long)total);
-    if (near) fill<FILL_THREADS>(p, entries, InShared{sh_start}, (int)begin, end);
-    else fill<FILL_THREADS>(p, entries, InGlobal{p.token_start}, (int)begin, end);
+    auto write = [&](const auto &starts) {
+        if (few) fill_singly<FILL_THREADS>(p, entries, starts, (int)begin, end);
+        else fill<FILL_THREADS>(p, entries, starts, (int)begin, end);
+    };
+    if (near) write(InShared{sh_start});
+    else write(InGlobal{p.token_start});
 }
 
 // A cluster per pool.  A warp takes a row of 32 sequences, or several, one behind the other; where there are more warps than rows,
@@ -586,9 +610,9 @@ template <int THREADS> __global__ void __launch_bounds__(THREADS) release_kernel
 size_t cache_workspace_bytes(int max_batch, int n_pools) { return (size_t)max_batch * sizeof(PlanEntry); }
 
 // Up to so many entries (that the outputs have room for) the planning cluster writes them too.  Us a plan and release on the device with one
-// launch and with two, and the entries there is room for and there are: one sequence, 64 and 3, 4.8 and 6.5; 1024 sequences, 9216 and 5 k,
-// 12.2 and 12.2; 333 sequences, 62 k and 16 k, 12.7 and 11.1; 256 sequences, 87 k and 26 k, 16.4 and 10.9.  A launch takes the host
-// 2.2 us.
+// launch and with two, and the entries there is room for and there are: 1024 sequences, 9216 and 5 k, 11.1 and 11.2; 333 sequences,
+// 62 k and 16 k, 12.6 and 10.5; 256 sequences, 87 k and 26 k, 18.6 and 10.2.  A launch takes the host 2.2 us, which eager calls wait for: 12.6
+// and 13.5 a pass of the second.
 constexpr int ALONE_ENTRIES = 65536, PLAN_CLUSTER = 8;
 // Releases of so many sequences take blocks of 256 threads, of more 1024: fewer warps are quicker where little comes back (1024
 // sequences, 11.5 us a plan and release instead of 12.4), more where much does (1024 x 96 blocks: 38 us instead of 47).
@@ -602,14 +626,14 @@ cudaError_t launch_cache_plan(const CachePlanParams &params, int n_sm, cudaStrea
     if (p.max_tokens <= ALONE_ENTRIES) {
         const int threads = small ? 256 : MOST_THREADS;
         int cluster = 1;
-        while (cluster < PLAN_CLUSTER && cluster * 2 * threads < p.max_tokens) cluster *= 2;
+        while (cluster < PLAN_CLUSTER && cluster * threads < p.max_tokens) cluster *= 2;
         return small ? launch_kernel(plan_kernel<256, true>, (unsigned)cluster, 256, 0, cluster, true, stream, p)
                      : launch_kernel(plan_kernel<MOST_THREADS, true>, (unsigned)cluster, MOST_THREADS, 0, cluster, true, stream, p);
     }
     cudaError_t e = small ? launch_kernel(plan_kernel<256, false>, 1, 256, 0, 1, true, stream, p)
                           : launch_kernel(plan_kernel<MOST_THREADS, false>, 1, MOST_THREADS, 0, 1, true, stream, p);
     if (e != cudaSuccess) return e;
-    const unsigned grid = (unsigned)std::min<long long>(((long long)p.max_tokens + 2 * FILL_THREADS - 1) / (2 * FILL_THREADS), (long long)FILL_BLOCKS * n_sm);
+    const unsigned grid = (unsigned)std::min<long long>(((long long)p.max_tokens + FILL_THREADS - 1) / FILL_THREADS, (long long)FILL_BLOCKS * n_sm);
     return launch_kernel(fill_kernel, grid, FILL_THREADS, 0, 1, true, stream, p);
 }
 
