@@ -331,12 +331,13 @@ __device__ __forceinline__ int crossing_lane(double x, double upto, double thres
 struct Crossing {
     double base, threshold;
     int g0, g1;         // the part's vectors
+    int found;          // the first token whose sum is beyond the threshold
     int last;           // the last token with weight so far, for sums that rounding leaves below the threshold
     bool again;         // nothing is left over of the target's row: it is drawn from as it stands
 };
 
-// By all threads, a vector each and a stretch of THREADS vectors at a time; returns to one thread the token, to the others -1.  A thread's
-// sums end, bit for bit, where the next one's begin: one of them holds the threshold, or none.
+// By all threads, a vector each and a stretch of THREADS vectors at a time; thread 0 has the token.  Every warp offers its first candidate and the
+// smallest is taken: sums of different lanes are rounded differently and need not rise from lane to lane by the last bit.
 template <typename LT>
 __device__ __forceinline__ int find_token(const PairOfRows<LT> &r, bool pair, Crossing &sh, double (&sh_warp)[WARPS])
 {
@@ -365,8 +366,6 @@ __device__ __forceinline__ int find_token(const PairOfRows<LT> &r, bool pair, Cr
         for (int e = 0; e < VEC; e += 2) add_pair<true, false>(x, pack2(p[e], p[e + 1]), pack2(q[e], q[e + 1]));
         const double mine = weight_of(x);
         const double upto = lanes_up_to(mine);
-        double start = __shfl_up_sync(FULL, upto, 1);
-        if (lane == 0) start = 0.0;
         if (lane == 31) sh_warp[warp] = upto;
         last = __reduce_max_sync(FULL, last);
         if (lane == 0 && last >= 0) atomicMax(&sh.last, last);
@@ -375,10 +374,10 @@ __device__ __forceinline__ int find_token(const PairOfRows<LT> &r, bool pair, Cr
         for (int i = 0; i < warp; ++i) offset += sh_warp[i];
         double end = offset;
         for (int i = warp; i < WARPS; ++i) end += sh_warp[i];
-        const bool mass = mine > 0.0, here = mass && offset + start <= threshold && offset + upto > threshold;
-        int token = -1;
-        if (here) {
-            double run = offset + start;
+        const unsigned hits = __ballot_sync(FULL, mine > 0.0 && offset + upto > threshold);
+        if (hits && lane == __ffs(hits) - 1) {
+            double run = offset + (upto - mine);
+            int token = -1;
             bool done = false;
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
@@ -389,8 +388,9 @@ __device__ __forceinline__ int find_token(const PairOfRows<LT> &r, bool pair, Cr
                     done = run > threshold;
                 }
             }
+            atomicMin(&sh.found, token);
         }
-        if (__syncthreads_or(here)) return token;
+        if (__syncthreads_or(hits != 0)) return tid == 0 ? sh.found : -1;
         base = end;
     }
     return tid == 0 ? sh.last : -1;
@@ -522,7 +522,7 @@ __global__ void __launch_bounds__(THREADS, 4) probs_kernel(const ProbsParams p)
             for (int i = 0; i < PER; ++i) mine += w[i];
             const double upto = lanes_up_to(mine), total = __shfl_sync(FULL, upto, 31);
             const bool bad = !(total < INFINITY);
-            Crossing x = {0.0, 0.0, 0, 0, -1, false};      // nothing to look for
+            Crossing x = {0.0, 0.0, 0, 0, 0x7FFFFFFF, -1, false};      // nothing to look for
             if (n == j) {       // the row that the token is drawn from
                 if (total > 0.0 && !bad) {
                     x.threshold = (double)u_draw * total;
@@ -579,7 +579,7 @@ __global__ void __launch_bounds__(THREADS, 4) probs_kernel(const ProbsParams p)
     }
     if (TV && n != j) return;
     const int token = find_token<LT>(r, pair, sh_crossing, sh_warp);
-    if (token >= 0 || (tid == 0 && sh_crossing.g0 == sh_crossing.g1)) p.next_token[b] = token;
+    if (tid == 0) p.next_token[b] = token;
 }
 
 // The reward of a round that metasd_verify did not verify, the bandit update and the next selection: a warp per sequence.
