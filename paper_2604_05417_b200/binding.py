@@ -27,6 +27,7 @@ STATUS_BAD_INDEX, STATUS_NO_BLOCKS, STATUS_TRUNCATED, STATUS_BAD_STATE = 64, 128
 OK, ERR_INVALID_ARGUMENT, ERR_UNSUPPORTED, ERR_CUDA, ERR_NO_MEMORY, ERR_BAD_STATE_BLOB = 0, -1, -2, -3, -4, -5
 
 BANDITS = {"ucb": UCB, "ducb": DUCB, "swucb": SWUCB, "exp3": EXP3, "rand": RAND, "petc": PETC}
+_I32, _I64, _F32, _BF16 = torch.int32, torch.int64, torch.float32, torch.bfloat16
 DTYPES = {"bf16": BF16, "fp32": FP32, torch.bfloat16: BF16, torch.float32: FP32}
 
 EXPORTS = (
@@ -211,17 +212,18 @@ def _expect_all(index: int, dtype, shape, **tensors):
 
 def _verify_probs(ctx, target, draft, tokens, u_accept, u_draw, draft_len, draft_place, seed, out, want_d_tv, status):
     dtype, index = target.dtype, target.get_device()
-    if index < 0 or target.dim() != 3 or (dtype is not torch.float32 and dtype is not torch.bfloat16):
+    shape = target.shape
+    if index < 0 or len(shape) != 3 or (dtype is not _F32 and dtype is not _BF16):
         raise ValueError("target_probs: a CUDA tensor [B, k + 1, V] of bf16 or fp32 is due")
     lib = _lib or load_library()
     are = _are if _call is None else _call.are
-    B, rows, V = target.shape
-    k, i32, f32, each = rows - 1, torch.int32, torch.float32, (B,)
+    B, rows, V = shape
+    k, each = rows - 1, (B,)
     tss, trs, entry = target.stride()
     if entry != 1 and V > 1:
         raise ValueError("target_probs: a row's entries have to lie next to each other (stride %d)" % entry)
     if out is None:
-        out = ProbsResult(torch.empty(each, dtype=i32, device=target.device), torch.empty(each, dtype=i32, device=target.device))
+        out = ProbsResult(torch.empty(each, dtype=_I32, device=target.device), torch.empty(each, dtype=_I32, device=target.device))
     accepted, token, d_tv, reward = out.accepted_len, out.next_token, None, None
     dss = drs = 0
     if k > 0:
@@ -235,31 +237,31 @@ def _verify_probs(ctx, target, draft, tokens, u_accept, u_draw, draft_len, draft
         if want_d_tv:
             d_tv = out.d_tv
             if d_tv is None:
-                d_tv = out.d_tv = torch.zeros(drafted, dtype=f32, device=target.device)
-        if tokens is None or not are(index, i32, drafted, tokens):
-            _refuse("draft_tokens", tokens, i32, drafted, index)
-        if u_accept is None or not are(index, f32, drafted, u_accept, d_tv):
-            _expect("u_accept", u_accept, f32, drafted, index)
-            _refuse("d_tv", d_tv, f32, drafted, index)
+                d_tv = out.d_tv = torch.zeros(drafted, dtype=_F32, device=target.device)
+        if tokens is None or not are(index, _I32, drafted, tokens):
+            _refuse("draft_tokens", tokens, _I32, drafted, index)
+        if u_accept is None or not are(index, _F32, drafted, u_accept, d_tv):
+            _expect("u_accept", u_accept, _F32, drafted, index)
+            _refuse("d_tv", d_tv, _F32, drafted, index)
     else:
         tokens = u_accept = draft = None
         if want_d_tv and out.d_tv is None:
-            out.d_tv = torch.zeros((B, 0), dtype=f32, device=target.device)
+            out.d_tv = torch.zeros((B, 0), dtype=_F32, device=target.device)
     if ctx is not None:
         reward = out.reward
         if reward is None:
-            reward = out.reward = torch.empty(each, dtype=f32, device=target.device)
-    if u_draw is None or not are(index, f32, each, u_draw, reward):
-        _expect("u_draw", u_draw, f32, each, index)
-        _refuse("reward", reward, f32, each, index)
-    if accepted is None or token is None or not are(index, i32, each, accepted, token, draft_len, draft_place):
-        _expect("accepted_len", accepted, i32, each, index)
-        _expect("next_token", token, i32, each, index)
-        _expect_all(index, i32, each, draft_len=draft_len, draft_place=draft_place)
+            reward = out.reward = torch.empty(each, dtype=_F32, device=target.device)
+    if u_draw is None or not are(index, _F32, each, u_draw, reward):
+        _expect("u_draw", u_draw, _F32, each, index)
+        _refuse("reward", reward, _F32, each, index)
+    if accepted is None or token is None or not are(index, _I32, each, accepted, token, draft_len, draft_place):
+        _expect("accepted_len", accepted, _I32, each, index)
+        _expect("next_token", token, _I32, each, index)
+        _expect_all(index, _I32, each, draft_len=draft_len, draft_place=draft_place)
     if status is not None:
-        _expect("status", status, i32, (1,), index)
+        _expect("status", status, _I32, (1,), index)
     stream = _raw_stream(index) if _raw_stream is not None else _stream(target.device)
-    args = (ctx, index, B, k, V, BF16 if dtype is torch.bfloat16 else FP32, target, tss, trs, draft, dss, drs, draft_place, tokens, draft_len,
+    args = (ctx, index, B, k, V, BF16 if dtype is _BF16 else FP32, target, tss, trs, draft, dss, drs, draft_place, tokens, draft_len,
             u_accept, u_draw, seed, accepted, token, d_tv, reward, status, stream)
     rc = NotImplemented
     if _call is not None:
@@ -508,7 +510,7 @@ class BlockCache:
              max_tokens: Optional[int] = None, out: Optional[CachePlan] = None) -> CachePlan:
         """metasd_cache_plan: length [B], cached [B] or [n_pools, B], pool [B] (None: pool 0), int32.  max_tokens: entries that the
         outputs have room for, where they are not given."""
-        index, i32 = self.index, torch.int32
+        index = self.index
         are = _are if _call is None else _call.are
         B = length.shape[0]
         each = (B,)
@@ -516,9 +518,9 @@ class BlockCache:
             if max_tokens is None:
                 raise ValueError("max_tokens or the outputs are due")
             def ints(*shape):
-                return torch.empty(shape, dtype=i32, device=self.device)
+                return torch.empty(shape, dtype=_I32, device=self.device)
             out = CachePlan(ints(B), ints(B), ints(self.n_pools + 1), ints(B + 1),
-                            torch.empty(max_tokens, dtype=torch.int64, device=self.device), ints(max_tokens), ints(max_tokens))
+                            torch.empty(max_tokens, dtype=_I64, device=self.device), ints(max_tokens), ints(max_tokens))
         order, place, pool_start, token_start = out.order, out.place, out.pool_start, out.token_start
         slot_map, position, sequence = out.slot_map, out.position, out.sequence
         room = slot_map.shape[0]
@@ -526,16 +528,16 @@ class BlockCache:
             raise ValueError("slot_map has room for %d entries, not %d" % (room, max_tokens))
         stride = 0 if cached.dim() == 1 else B
         # one question for each type and shape; who is not what is due is found where the answer is no
-        if not (are(index, i32, each, length, pool, order, place, None if stride else cached) and
-                (stride == 0 or are(index, i32, (self.n_pools, B), cached)) and are(index, i32, (B + 1,), token_start) and
-                token_start is not None and are(index, torch.int64, (room,), slot_map) and are(index, i32, (room,), position, sequence) and
-                are(index, i32, (self.n_pools + 1,), pool_start)):
-            _expect_all(index, i32, each, length=length, pool=pool, order=order, place=place)
-            _expect("cached", cached, i32, (self.n_pools, B) if stride else each, index)
-            _expect("token_start", token_start, i32, (B + 1,), index)
-            _expect("slot_map", slot_map, torch.int64, (room,), index)
-            _expect_all(index, i32, (room,), position=position, sequence=sequence)
-            _expect_all(index, i32, (self.n_pools + 1,), pool_start=pool_start)
+        if not (are(index, _I32, each, length, pool, order, place, None if stride else cached) and
+                (stride == 0 or are(index, _I32, (self.n_pools, B), cached)) and are(index, _I32, (B + 1,), token_start) and
+                token_start is not None and are(index, _I64, (room,), slot_map) and are(index, _I32, (room,), position, sequence) and
+                are(index, _I32, (self.n_pools + 1,), pool_start)):
+            _expect_all(index, _I32, each, length=length, pool=pool, order=order, place=place)
+            _expect("cached", cached, _I32, (self.n_pools, B) if stride else each, index)
+            _expect("token_start", token_start, _I32, (B + 1,), index)
+            _expect("slot_map", slot_map, _I64, (room,), index)
+            _expect_all(index, _I32, (room,), position=position, sequence=sequence)
+            _expect_all(index, _I32, (self.n_pools + 1,), pool_start=pool_start)
         args = (self._at, B, pool, cached, stride, length, room, order, place, pool_start, token_start, slot_map, position, sequence,
                 _raw_stream(index) if _raw_stream is not None else _stream(self.device))
         rc = NotImplemented
@@ -552,7 +554,7 @@ class BlockCache:
         index, B = self.index, keep.shape[-1]
         stride = 0 if keep.dim() == 1 else B
         shape = (self.n_pools, B) if stride else (B,)
-        if not (_are if _call is None else _call.are)(index, torch.int32, shape, keep):
+        if not (_are if _call is None else _call.are)(index, _I32, shape, keep):
             _refuse("keep", keep, torch.int32, shape, index)
         args = (self._at, B, keep, stride, _raw_stream(index) if _raw_stream is not None else _stream(self.device))
         rc = NotImplemented
