@@ -15,7 +15,7 @@
 //
 // A release gives back what lies beyond the entries that stay, to the end of the free list, in the order that lets the next plan
 // take the same blocks for the same places: one cluster per pool, bound by latency too (2.1 us for one sequence, 3.3 for 1024 with
-// nothing to give back, 9 for 98 304 blocks).
+// nothing to give back, 7 for 98 304 blocks).
 #include <algorithm>
 
 #include "metasd_staged.cuh"
@@ -515,8 +515,10 @@ __global__ void __launch_bounds__(FILL_THREADS, FILL_BLOCKS) fill_kernel(const C
 }
 
 // A cluster per pool.  A warp takes a row of 32 sequences, or several, one behind the other; where there are more warps than rows,
-// several share a row's blocks.  Blocks are copied one by one over all lanes, whatever sequence they come from.
+// several share a row's blocks.  A few blocks are copied over all lanes at once, whatever sequence they come from; many one sequence after
+// the other, with less to do for each.
 constexpr int RELEASE_CLUSTER = 8, RELEASE_GROUPS = RELEASE_CLUSTER * MOST_WARPS, AT_ONCE = 4;
+constexpr int MANY = 256;       // blocks that a row of sequences gives back: 1024 x 96 37.4 -> 35.2 us a plan and release; 64 .. 1024 as good
 
 template <int THREADS> __global__ void __launch_bounds__(THREADS) release_kernel(const CacheReleaseParams p)
 {
@@ -576,7 +578,7 @@ template <int THREADS> __global__ void __launch_bounds__(THREADS) release_kernel
             if (row1 - row0 > 1) drop = look(row, from);
             const int upto = warp_sum_up_to(drop), n = __shfl_sync(FULL, upto, 31);
             const long long top = free + total - 1 - before;
-            for (int e0 = 32 * sub; e0 < n; e0 += 32 * share * AT_ONCE) {
+            for (int e0 = 32 * sub; e0 < n && n < MANY; e0 += 32 * share * AT_ONCE) {
                 int id[AT_ONCE];
 #pragma unroll
                 for (int i = 0; i < AT_ONCE; ++i) {
@@ -593,6 +595,19 @@ template <int THREADS> __global__ void __launch_bounds__(THREADS) release_kernel
                 for (int i = 0; i < AT_ONCE; ++i) {
                     const int e = e0 + 32 * share * i + lane;
                     if (e < n) list[top - e] = id[i];
+                }
+            }
+            for (int s = sub; s < 32 && n >= MANY; s += share) {        // much to give back: one sequence after the other
+                const int d = __shfl_sync(FULL, drop, s), ahead = __shfl_sync(FULL, upto - drop, s);
+                const int32_t *source = tables + (int64_t)(row * 32 + s) * c.max_blocks + __shfl_sync(FULL, from, s);
+                int32_t *to = list + (top - ahead);
+                for (int e0 = lane; e0 < d; e0 += 32 * AT_ONCE) {
+                    int id[AT_ONCE];
+#pragma unroll
+                    for (int i = 0; i < AT_ONCE; ++i) id[i] = e0 + 32 * i < d ? source[e0 + 32 * i] : 0;
+#pragma unroll
+                    for (int i = 0; i < AT_ONCE; ++i)
+                        if (e0 + 32 * i < d) to[-(e0 + 32 * i)] = id[i];
                 }
             }
             before += n;
@@ -615,7 +630,7 @@ size_t cache_workspace_bytes(int max_batch, int n_pools) { return (size_t)max_ba
 // and 13.5 a pass of the second.
 constexpr int ALONE_ENTRIES = 65536, PLAN_CLUSTER = 8;
 // Releases of so many sequences take blocks of 256 threads, of more 1024: fewer warps are quicker where little comes back (1024
-// sequences, 11.5 us a plan and release instead of 12.4), more where much does (1024 x 96 blocks: 38 us instead of 47).
+// sequences, 10.4 us a plan and release instead of 11.1), more where much does (1024 x 96 blocks: 35.4 us instead of 41.5).
 constexpr int SMALL_RELEASE = 512;
 
 cudaError_t launch_cache_plan(const CachePlanParams &params, int n_sm, cudaStream_t stream)
