@@ -186,9 +186,9 @@ class ProbsResult:
     reward: Optional[torch.Tensor] = None   # [B] fp32, of a context's round
 
 
-def _refuse(name: str, t, dtype, shape, index: int):
-    raise ValueError("%s: a contiguous %s tensor of shape %s on cuda:%d is due, not %s" % (
-        name, dtype, tuple(shape), index, "%s of shape %s on %s" % (t.dtype, tuple(t.shape), t.device)
+def _refuse(name: str, t, dtype, shape, index: int, kind: str = "contiguous "):
+    raise ValueError("%s: a %s%s tensor of shape %s on cuda:%d is due, not %s" % (
+        name, kind, dtype, tuple(shape), index, "%s of shape %s on %s" % (t.dtype, tuple(t.shape), t.device)
         if isinstance(t, torch.Tensor) else type(t).__name__))
 
 
@@ -230,7 +230,7 @@ def _verify_probs(ctx, target, draft, tokens, u_accept, u_draw, draft_len, draft
         drafted = (B, k)
         if draft is not None:
             if draft.dtype is not dtype or draft.shape != (B, k, V) or draft.get_device() != index:
-                _refuse("draft_probs", draft, dtype, (B, k, V), index)
+                _refuse("draft_probs", draft, dtype, (B, k, V), index, "")
             dss, drs, entry = draft.stride()
             if entry != 1 and V > 1:
                 raise ValueError("draft_probs: a row's entries have to lie next to each other (stride %d)" % entry)

@@ -14,7 +14,7 @@
 // pair.  512 sequences of 152064 fp32 entries without: 93 us, 6.6 TB/s; 256 x 7 pairs of 128256 bf16 entries with: 148 us, 6.3 TB/s
 // (a copy makes 6.5).  Small calls are a chain: the accept tests' two dependent loads 1.0 us, a part 1.1, the blocks' meeting 0.6, the
 // parts' sums and the draw 1.5; one sequence of 32000 entries 4.9 us.
-//  A row is cut into parts by its length alone, a warp sums a part, and the parts' sums are put together in one order:
+// A row is cut into parts by its length alone, a warp sums a part, and the parts' sums are put together in one order:
 // results do not depend on the launch's shape, and the draw re-reads one part (of 80 to 160 of a long row) and not the row.
 #include <algorithm>
 

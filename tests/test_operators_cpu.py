@@ -107,6 +107,23 @@ def test_calls_convert_as_ctypes_does(lib):
             fn(*args[:-1])
 
 
+def test_tensors_are_checked_alike_with_and_without_the_extension_module(lib):
+    """Type, shape, device (-1: the host) and contiguity, of every tensor that is not None; what is no tensor is an AttributeError."""
+    t = torch.zeros((4, 3), dtype=torch.int32)
+    for are in [M._are] + ([M._call.are] if M._call is not None else []):
+        assert are(-1, torch.int32, (4, 3)) and are(-1, torch.int32, (4, 3), None, t, t.clone())
+        assert are(-1, torch.int32, (0,), torch.zeros(0, dtype=torch.int32)) and are(-1, torch.int32, (3,), t[1])
+        for bad in (t.long(), t[:, :2], t[0], t.t(), t.t().contiguous(), torch.zeros((4, 6), dtype=torch.int32)[:, ::2], t.float()):
+            assert not are(-1, torch.int32, (4, 3), t, bad)
+        assert not are(0, torch.int32, (4, 3), t)       # on another device
+        with pytest.raises(AttributeError):
+            are(-1, torch.int32, (4, 3), t, 12345)
+    with pytest.raises(ValueError, match="keep: a contiguous torch.int32 tensor of shape .4, 3. on cuda:0 is due, not torch.int64"):
+        M._expect("keep", t.long(), torch.int32, (4, 3), 0)
+    with pytest.raises(ValueError, match="is due, not NoneType"):
+        M._expect("keep", None, torch.int32, (4, 3), 0)
+
+
 def test_reference_verification_by_hand():
     p = np.array([[[0.5, 0.25, 0.25], [0.0, 1.0, 0.0]]])
     q = np.array([[[0.25, 0.75, 0.0]]])
