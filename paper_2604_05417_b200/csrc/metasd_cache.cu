@@ -625,10 +625,9 @@ template <int THREADS> __global__ void __launch_bounds__(THREADS) release_kernel
 size_t cache_workspace_bytes(int max_batch, int n_pools) { return (size_t)max_batch * sizeof(PlanEntry); }
 
 // Up to so many entries (that the outputs have room for) the planning cluster writes them too.  Us a plan and release on the device with one
-// launch and with two, and the entries there is room for and there are: 1024 sequences, 9216 and 5 k, 11.1 and 11.2; 333 sequences,
-// 62 k and 16 k, 12.6 and 10.5; 256 sequences, 87 k and 26 k, 18.6 and 10.2.  A launch takes the host 2.2 us, which eager calls wait for: 12.6
-// and 13.5 a pass of the second.
-constexpr int ALONE_ENTRIES = 65536, PLAN_CLUSTER = 8;
+// launch and with two, and the entries there is room for and there are: 1024 sequences, 9216 and 5 k, 11.1 and 11.2 (a launch takes the host
+// 2.2 us besides); 333 sequences, 62 k and 16 k, 12.6 and 10.5; 256 sequences, 87 k and 26 k, 18.6 and 10.2.
+constexpr int ALONE_ENTRIES = 16384, PLAN_CLUSTER = 8;
 // Releases of so many sequences take blocks of 256 threads, of more 1024: fewer warps are quicker where little comes back (1024
 // sequences, 10.4 us a plan and release instead of 11.1), more where much does (1024 x 96 blocks: 35.4 us instead of 41.5).
 constexpr int SMALL_RELEASE = 512;
