@@ -518,6 +518,7 @@ __global__ void __launch_bounds__(FILL_THREADS, FILL_BLOCKS) fill_kernel(const C
 // several share a row's blocks.  A few blocks are copied over all lanes at once, whatever sequence they come from; many one sequence after
 // the other, with less to do for each.
 constexpr int RELEASE_CLUSTER = 8, RELEASE_GROUPS = RELEASE_CLUSTER * MOST_WARPS, AT_ONCE = 4;
+constexpr int LONG = 1024;      // blocks of a table from which a release takes all the warps there are
 constexpr int MANY = 256;       // blocks that a row of sequences gives back: 1024 x 96 37.4 -> 35.2 us a plan and release; 64 .. 1024 as good
 
 template <int THREADS> __global__ void __launch_bounds__(THREADS) release_kernel(const CacheReleaseParams p)
@@ -597,18 +598,25 @@ template <int THREADS> __global__ void __launch_bounds__(THREADS) release_kernel
                     if (e < n) list[top - e] = id[i];
                 }
             }
-            for (int s = sub; s < 32 && n >= MANY; s += share) {        // much to give back: one sequence after the other
-                const int d = __shfl_sync(FULL, drop, s), ahead = __shfl_sync(FULL, upto - drop, s);
-                const int32_t *source = tables + (int64_t)(row * 32 + s) * c.max_blocks + __shfl_sync(FULL, from, s);
-                int32_t *to = list + (top - ahead);
-                for (int e0 = lane; e0 < d; e0 += 32 * AT_ONCE) {
-                    int id[AT_ONCE];
+            if (n >= MANY) {
+                // Much to give back: the row's warps take a sequence each, and share those that are more than twice a warp's part.
+                auto give = [&](int s, int begin, int by) {
+                    const int d = __shfl_sync(FULL, drop, s), ahead = __shfl_sync(FULL, upto - drop, s), first = __shfl_sync(FULL, from, s);
+                    const int32_t *source = tables + (int64_t)(row * 32 + s) * c.max_blocks + first;
+                    int32_t *to = list + (top - ahead);
+                    for (int e0 = begin; e0 < d; e0 += by * AT_ONCE) {
+                        int id[AT_ONCE];
 #pragma unroll
-                    for (int i = 0; i < AT_ONCE; ++i) id[i] = e0 + 32 * i < d ? source[e0 + 32 * i] : 0;
+                        for (int i = 0; i < AT_ONCE; ++i) id[i] = e0 + by * i < d ? source[e0 + by * i] : 0;
 #pragma unroll
-                    for (int i = 0; i < AT_ONCE; ++i)
-                        if (e0 + 32 * i < d) to[-(e0 + 32 * i)] = id[i];
-                }
+                        for (int i = 0; i < AT_ONCE; ++i)
+                            if (e0 + by * i < d) to[-(e0 + by * i)] = id[i];
+                    }
+                };
+                unsigned shared = __ballot_sync(FULL, (long long)drop * share > 2ll * n);
+                for (int s = sub; s < 32; s += share)
+                    if (!(shared >> s & 1u)) give(s, lane, 32);
+                for (; shared; shared &= shared - 1u) give(__ffs(shared) - 1, lane + 32 * sub, 32 * share);
             }
             before += n;
             __syncwarp();
@@ -629,7 +637,8 @@ size_t cache_workspace_bytes(int max_batch, int n_pools) { return (size_t)max_ba
 // 2.2 us besides); 333 sequences, 62 k and 16 k, 12.6 and 10.5; 256 sequences, 87 k and 26 k, 18.6 and 10.2.
 constexpr int ALONE_ENTRIES = 16384, PLAN_CLUSTER = 8;
 // Releases of so many sequences take blocks of 256 threads, of more 1024: fewer warps are quicker where little comes back (1024
-// sequences, 10.4 us a plan and release instead of 11.1), more where much does (1024 x 96 blocks: 35.4 us instead of 41.5).
+// sequences, 10.4 us a plan and release instead of 11.1), more where much does (1024 x 96 blocks: 35.4 us instead of 41.5), or may: tables
+// of more than LONG blocks take all there is (45 sequences, tables of 10 k blocks, of which 70 k come back: 14.3 us instead of 48).
 constexpr int SMALL_RELEASE = 512;
 
 cudaError_t launch_cache_plan(const CachePlanParams &params, int n_sm, cudaStream_t stream)
@@ -655,8 +664,8 @@ cudaError_t launch_cache_release(const CacheReleaseParams &params, cudaStream_t 
 {
     CacheReleaseParams p = params;
     const int rows = (p.batch + 31) / 32;
-    const bool small = p.batch <= SMALL_RELEASE;
-    int cluster = 1;
+    const bool small = p.batch <= SMALL_RELEASE && p.c.max_blocks <= LONG;
+    int cluster = p.c.max_blocks <= LONG ? 1 : RELEASE_CLUSTER;
     while (cluster < RELEASE_CLUSTER && cluster * (small ? 32 : 128) < p.batch) cluster *= 2;
     p.share = cluster * (small ? 8 : MOST_WARPS) / rows;
     p.share_inverse = inverse_of((uint32_t)std::max(p.share, 1));

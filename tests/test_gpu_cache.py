@@ -132,6 +132,28 @@ def test_tables_beyond_32_bits():
     assert torch.equal(cache.free_blocks[0], cache.free_blocks[1]) and int(cache.held.sum()) == 0
 
 
+@pytest.mark.parametrize("batch,pools,page,longest", [(3, 2, 1, 5000), (45, 1, 1, 3000), (200, 2, 1, 1500), (700, 1, 2, 700), (70, 3, 3, 3100)])
+def test_releases_of_uneven_tables(batch, pools, page, longest):
+    """A few long tables among short and empty ones: a row's blocks given back by one warp each, and by all together."""
+    rng = np.random.default_rng(longest)
+    most = -(-longest // page)
+    cache, ref = pair(pools, batch, most, batch * most // 4 + 4 * most, page, seed=batch)
+    for t in range(3):
+        goal = np.where(rng.random(batch) < 0.1, rng.integers(longest // 2, longest + 1, size=batch), rng.integers(0, 40, size=batch))
+        goal[rng.random(batch) < 0.4] = 0
+        for g in range(pools):
+            have = np.array([[len(ref.table[i][b]) * page for b in range(batch)] for i in range(pools)])
+            plan_both(cache, ref, np.maximum(goal, have[g]), have, np.full(batch, g))
+        keep = np.where(rng.random((pools, batch)) < 0.5, 0, rng.integers(0, longest, size=(pools, batch)))
+        cache.release(ints(keep))
+        ref.release(keep)
+        same(cache, ref)
+    cache.release(ints(np.zeros(batch)))
+    ref.release(np.zeros((pools, batch)))
+    same(cache, ref)
+    assert cache.last_status() in (0, M.STATUS_NO_BLOCKS)
+
+
 def test_a_release_undoes_a_plan():
     cache, ref = pair(4, 50, 30, 800, 8, seed=3)
     rng = np.random.default_rng(3)
