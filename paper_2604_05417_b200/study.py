@@ -154,6 +154,23 @@ def cut_probabilities(logits: torch.Tensor, temperature: float, min_p: float) ->
     return p
 
 
+def has_slots(plan: M.CachePlan) -> torch.Tensor:
+    """[B]: whether the plan has slots for the entries that a sequence adds (one at least); its pool may have had too few blocks."""
+    return plan.slot_map[plan.token_start[plan.place.long()].long()] >= 0
+
+
+def advance(plan_d: M.CachePlan, plan_t: M.CachePlan, arm: torch.Tensor, length: torch.Tensor, accepted: torch.Tensor, goal_d: torch.Tensor,
+            in_drafters: torch.Tensor, in_target: torch.Tensor):
+    """What is cached behind a round, and the sequences' lengths: in_drafters [N, B], in_target [B], length [B].  A cache whose plan had no
+    slots for a sequence holds what it held: the round's entries were not kept, and the next plan has them again."""
+    at, played = torch.arange(length.shape[0], device=length.device), arm.long()
+    stays = length + accepted           # the accepted drafts; the token behind them has been through no model
+    had = in_drafters[played, at]
+    in_drafters = in_drafters.clone()
+    in_drafters[played, at] = torch.where(has_slots(plan_d), torch.maximum(had, torch.minimum(goal_d, stays)), had)
+    return in_drafters, torch.where(has_slots(plan_t), stays, in_target), stays + 1
+
+
 def serving_rounds(wl: Workload, rounds: int, bandit: str, device=0, seed: int = 0, min_p: float = 0.02, page: int = 16, longest: int = 400,
                    pool_blocks: Optional[int] = None):
     """The serving loop of Algorithm 1 around the library: per round the drafters are selected, the drafters' and the target's caches are
@@ -162,7 +179,8 @@ def serving_rounds(wl: Workload, rounds: int, bandit: str, device=0, seed: int =
     loop's own and change with the next one.
 
     Of a sequence with `length` tokens the target's cache holds all but the last.  A drafter that is chosen brings its own cache up to
-    date and adds its drafts but the last; of these the accepted ones stay.  A query ends at `longest` tokens: its bandit starts anew
+    date and adds its drafts but the last; of these the accepted ones stay.  Where a pool has too few blocks (pool_blocks) for a sequence, the
+    round's entries of its cache are not kept and are planned again with the next round's.  A query ends at `longest` tokens: its bandit starts anew
     and a prompt of another length takes its place."""
     dev, i32 = torch.device("cuda", device), torch.int32
     B, N, k = wl.B, wl.N, wl.k
@@ -184,7 +202,6 @@ def serving_rounds(wl: Workload, rounds: int, bandit: str, device=0, seed: int =
     try:
         for t in range(rounds):
             arm = msd.select()
-            played = arm.long()
             goal_d, goal_t = length + (k - 1), length + k
             plan_d = drafters.plan(goal_d, in_drafters, pool=arm, max_tokens=room)
             plan_t = target.plan(goal_t, in_target, max_tokens=room)
@@ -198,10 +215,7 @@ def serving_rounds(wl: Workload, rounds: int, bandit: str, device=0, seed: int =
             yield dict(t=t, arm=arm, length=length, in_drafters=in_drafters, in_target=in_target, goal_d=goal_d, goal_t=goal_t, plan_d=plan_d,
                        plan_t=plan_t, target=p, draft=q, tokens=tokens, u_accept=u, u_draw=v, result=res, msd=msd, drafters=drafters,
                        target_cache=target, best_arm=gen.best_arm(t))
-            in_target = length + res.accepted_len
-            in_drafters = in_drafters.clone()
-            in_drafters[played, at] = torch.maximum(in_drafters[played, at], torch.minimum(goal_d, in_target))
-            length = in_target + 1
+            in_drafters, in_target, length = advance(plan_d, plan_t, arm, length, res.accepted_len, goal_d, in_drafters, in_target)
             done = length >= longest
             length = torch.where(done, prompts(), length)
             in_target = torch.where(done, 0, in_target)

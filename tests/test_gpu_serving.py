@@ -85,3 +85,31 @@ def test_serving_loop_that_runs_out_of_blocks():
         if r["t"] == 0:
             assert r["target_cache"].last_status() == M.STATUS_NO_BLOCKS
             assert (r["plan_t"].slot_map[:int(r["plan_t"].token_start[-1])] == -1).any()
+
+
+def test_sequences_without_blocks_are_planned_again():
+    """What had no slots is not taken for cached: no cache holds more entries than its blocks have room for, every plan has the entries
+    that its sequences lack, and sequences that went without get their slots in later rounds of the same query."""
+    wl, page = workload(B=12), 4
+    waiting, last = np.zeros(wl.B, bool), None
+    went_without = got_them_later = 0
+    for r in study.serving_rounds(wl, 25, "ucb", page=page, longest=60, pool_blocks=60):
+        arm, at = r["arm"].cpu().numpy(), np.arange(wl.B)
+        in_target = r["in_target"].cpu().numpy()
+        if last is not None:        # the target's cache behind a round without slots: as it was, or the query ended
+            assert np.all((in_target == last) | (in_target == 0) | ~waiting)
+            waiting &= in_target == last
+        for cache, plan, goal, cached in ((r["drafters"], r["plan_d"], r["goal_d"], r["in_drafters"]),
+                                          (r["target_cache"], r["plan_t"], r["goal_t"], r["in_target"][None])):
+            assert cache.last_status() in (0, M.STATUS_NO_BLOCKS)
+            held, cached, goal = (x.cpu().numpy() for x in (cache.held, cached, goal))
+            assert np.all(cached <= held * page)
+            row = arm if len(held) > 1 else 0 * arm
+            start, place = plan.token_start.cpu().numpy(), plan.place.cpu().numpy()
+            assert np.array_equal(start[place + 1] - start[place], goal - cached[row, at])
+            served = plan.slot_map.cpu().numpy()[start[place]] >= 0
+            assert np.array_equal(served, held[row, at] * page >= goal)
+        got_them_later += int((waiting & served).sum())     # of the target's cache
+        went_without += int((~served).sum())
+        waiting, last = ~served, in_target
+    assert went_without > 0 and got_them_later > 0

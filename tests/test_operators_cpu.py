@@ -1,6 +1,7 @@
 """Refusals of metasd_verify_probs, metasd_cache_plan and metasd_cache_release, on the host: before any CUDA call, so that they are
 the same with and without a device; and the plain walks that the GPU tests compare with, on cases worked by hand."""
 import ctypes as C
+from types import SimpleNamespace
 
 import numpy as np
 import pytest
@@ -10,6 +11,7 @@ import _probs_reference as R
 from _cache_reference import Caches
 from paper_2604_05417_b200 import binding as M
 from paper_2604_05417_b200 import build as B
+from paper_2604_05417_b200 import study
 
 
 @pytest.fixture(scope="module")
@@ -145,3 +147,42 @@ def test_reference_caches_by_hand():
     assert [e[0] for e in entries] == [48, 84, 85, 86, 87, 80, -1, -1]
     c.release([[0, 1, 0], [4, 0, 0]])
     assert c.free == [[10, 11], [20]] and c.table[1][0] == [21]
+
+
+@pytest.mark.parametrize("seed", range(3))
+def test_serving_bookkeeping_where_pools_run_out(seed):
+    """The serving loop's lengths over plans by the plain walk: caches never count entries that had no slots, so that every plan has the entries
+    that its sequences lack."""
+    rng = np.random.default_rng(seed)
+    N, B, k, page, longest, blocks = 3, 12, 4, 4, 60, 60
+    refs = [Caches(n, B, (longest + 2 * k) // page + 1, page, [list(range(blocks))] * n) for n in (N, 1)]
+
+    def ints(x):
+        return torch.as_tensor(np.asarray(x), dtype=torch.int32)
+
+    def prompts():
+        return ints(rng.integers(8, longest // 2, B))
+
+    length, in_drafters, in_target = prompts(), torch.zeros((N, B), dtype=torch.int32), torch.zeros(B, dtype=torch.int32)
+    went_without = 0
+    for t in range(40):
+        arm, accepted = ints(rng.integers(0, N, B)), ints(rng.integers(0, k + 1, B))
+        goal_d, goal_t = length + (k - 1), length + k
+        plans = []
+        for ref, goal, cached, pool in ((refs[0], goal_d, in_drafters, arm), (refs[1], goal_t, in_target[None], torch.zeros_like(arm))):
+            order, place, _, start, entries = ref.plan(goal.tolist(), cached.tolist(), pool.tolist())
+            place, start = torch.tensor(place), torch.tensor(start)
+            assert torch.equal(start[place + 1] - start[place], (goal - cached[pool.long(), torch.arange(B)]).long())
+            plans.append(SimpleNamespace(place=place, token_start=start, slot_map=torch.tensor([e[0] for e in entries])))
+            served = study.has_slots(plans[-1])
+            assert [len(ref.table[g][b]) * page >= goal[b] for b, g in enumerate(pool.tolist())] == served.tolist()
+            went_without += int((~served).sum())
+        before = in_target
+        in_drafters, in_target, after = study.advance(*plans, arm, length, accepted, goal_d, in_drafters, in_target)
+        assert torch.equal(after, length + accepted + 1) and torch.equal(in_target, torch.where(served, length + accepted, before))
+        done = after >= longest
+        length = torch.where(done, prompts(), after)
+        in_target, in_drafters = torch.where(done, 0, in_target), torch.where(done, 0, in_drafters)
+        refs[0].release(in_drafters.tolist())
+        refs[1].release(in_target[None].tolist())
+    assert went_without > 0
