@@ -8,7 +8,9 @@
 // Whole numbers come out of sums over a row, so the sums are made as if in real numbers: with d = fl(p - q) the rounding error
 // (p - d) - q of a difference that is above zero is a float, exactly (p >= q >= 0), and so is the rounding error of an addition
 // (Knuth's two-sum, six operations on a packed pair).  The errors, 2^-24 of what they belong to, are added up apart; what is lost
-// is theirs, below 2^-45 of the sum, and next to no draw is that near to an edge.  The lanes' sums join in fp64.
+// is theirs.  Of n additions that come to S the errors' sum is at most (i + 1) 2^-24 S after the i-th, which rounds it twice: all in all
+// less than (n^2 + 3n) 2^-48 S.  No chain is longer than n = 32, which bounds the loss by 2^-37 of the sum, and next to no draw is that near
+// to an edge.  Chains and lanes join in fp64.
 //
 // Bound by memory: without distances one row pair per sequence is read (the one that the token is drawn from), with them every
 // pair.  512 sequences of 152064 fp32 entries without: 93 us, 6.6 TB/s; 256 x 7 pairs of 128256 bf16 entries with: 148 us, 6.3 TB/s
@@ -28,6 +30,9 @@ constexpr int THREADS = 256, WARPS = THREADS / 32;
 constexpr int MAX_PARTS = 160;      // of a row; 5 per lane of the warp that looks for the crossing.  With 256 (8 a lane) that takes longer: 128256 fp32
                                     // lookups 13.1 us instead of 12.2, 512 rows of 152064 the same; with 128, 4 x 8 pairs of 152064 bf16 12.5 instead of 11.7
 constexpr int BATCH = 4;            // vectors of a row that a lane has in flight
+constexpr int CHAIN = 32;           // additions of a lane to one sum, at most (V up to 327680).  Longer parts add every batch's sums up in fp64, which costs
+                                    // registers: in all rows 256 x 7 pairs of 128256 bf16 took 150.1 us instead of 148.7, 256 draws of 32001 9.9 instead
+                                    // of 9.6, 64 lookups in 128256 fp32 12.15 instead of 11.75
 constexpr unsigned FULL = 0xFFFFFFFFu;
 
 // A pair of rows as 16-byte vectors: vector g of the row holds entries g VEC .. g VEC + VEC - 1.
@@ -235,19 +240,18 @@ __device__ __forceinline__ void add_batch(Sums &s, const uint4 (&ra)[BATCH], con
 }
 
 // A warp's sums of a part, put where the sequence's sums are collected.
-template <bool WEIGHT, bool TV> __device__ __forceinline__ void publish(const Sums &x, double lane_apart, int s, uint32_t weights_at, uint32_t apart_at)
+template <bool WEIGHT, bool TV>
+__device__ __forceinline__ void publish(bool lane_bad, double lane_weight, double lane_apart, int s, uint32_t weights_at, uint32_t apart_at)
 {
-    const double w = WEIGHT ? warp_sum(weight_of(x)) : 0.0;
+    const double w = WEIGHT ? warp_sum(lane_weight) : 0.0;
     const float apart = TV ? warp_sum_f((float)lane_apart) : 0.f;
-    const bool bad = __any_sync(FULL, x.bad);
+    const bool bad = __any_sync(FULL, lane_bad);
     if ((threadIdx.x & 31) == 0) {
         st_cluster(weights_at + 8u * s, bad ? (double)NAN : w);
         if (TV) st_cluster(apart_at + 4u * s, __float_as_int(bad ? NAN : apart));
     }
 }
 
-// The parts s0, s0 + step, .. below s1 of a row (pair), by one warp.  The order of additions does not depend on where the rows
-// start, and the sums that a draw needs (WEIGHT) do not change those of the distance.
 // Asks L2 for a batch: 2 KB of each row, a line per lane.
 template <typename LT> __device__ __forceinline__ void prefetch_batch(const PairOfRows<LT> &r, bool pair, int c)
 {
@@ -256,7 +260,9 @@ template <typename LT> __device__ __forceinline__ void prefetch_batch(const Pair
     if ((lane < 16 || pair) && g < r.n_vec) asm volatile("prefetch.global.L2 [%0];" ::"l"(row + g));
 }
 
-template <typename LT, bool PAIR, bool WEIGHT, bool TV, bool SHIFTED>
+// The parts s0, s0 + step, .. below s1 of a row (pair), by one warp.  The order of additions does not depend on where the rows
+// start, and the sums that a draw needs (WEIGHT) do not change those of the distance.  LONG: parts of chains above CHAIN.
+template <typename LT, bool PAIR, bool WEIGHT, bool TV, bool LONG, bool SHIFTED>
 __device__ __forceinline__ void sum_parts(const PairOfRows<LT> r, int part_vecs, int s0, int s1, int step, uint32_t weights_at, uint32_t apart_at)
 {
     constexpr int VEC = Logit<LT>::VEC;
@@ -264,11 +270,17 @@ __device__ __forceinline__ void sum_parts(const PairOfRows<LT> r, int part_vecs,
     for (int s = s0; s < s1; s += step) {
         const int g0 = s * part_vecs, g1 = min(g0 + part_vecs, r.n_vec);
         Sums x;
-        double apart = 0.0;
+        double weight = 0.0, apart = 0.0;
         auto fold = [&] {       // no chain of fp32 additions is longer than a batch
             if (TV) {
                 apart += (double)(x.apart + x.apart1);
                 x.apart = x.apart1 = 0.f;
+            }
+        };
+        auto fold_weight = [&] {
+            if (WEIGHT && LONG) {
+                weight += weight_of(x);
+                x.over = x.rest = 0ull;
             }
         };
         int c = g0;
@@ -285,6 +297,7 @@ __device__ __forceinline__ void sum_parts(const PairOfRows<LT> r, int part_vecs,
             if (SHIFTED) realign<LT>(ra, behind_a, r.lead_a);
             add_batch<LT, PAIR, WEIGHT, TV>(x, ra, PAIR ? rd : ra, c, r.certain);
             fold();
+            fold_weight();
         }
         // the row's end
 #pragma unroll 1
@@ -294,19 +307,19 @@ __device__ __forceinline__ void sum_parts(const PairOfRows<LT> r, int part_vecs,
             add_vectors<LT, PAIR, WEIGHT, TV>(x, ra, rd, g * VEC, r.certain);
         }
         fold();
-        publish<WEIGHT, TV>(x, apart, s, weights_at, apart_at);
+        publish<WEIGHT, TV>(x.bad, WEIGHT ? weight + weight_of(x) : 0.0, apart, s, weights_at, apart_at);
     }
 }
 
-template <typename LT, bool WEIGHT, bool TV>
+template <typename LT, bool WEIGHT, bool TV, bool LONG>
 __device__ __forceinline__ void sum_parts(const PairOfRows<LT> &r, bool pair, int part_vecs, int s0, int s1, int step, uint32_t weights_at, uint32_t apart_at)
 {
     if (pair) {
-        if ((r.lead_a | r.lead_d) == 0) sum_parts<LT, true, WEIGHT, TV, false>(r, part_vecs, s0, s1, step, weights_at, apart_at);
-        else sum_parts<LT, true, WEIGHT, TV, true>(r, part_vecs, s0, s1, step, weights_at, apart_at);
+        if ((r.lead_a | r.lead_d) == 0) sum_parts<LT, true, WEIGHT, TV, LONG, false>(r, part_vecs, s0, s1, step, weights_at, apart_at);
+        else sum_parts<LT, true, WEIGHT, TV, LONG, true>(r, part_vecs, s0, s1, step, weights_at, apart_at);
     } else {
-        if (r.lead_a == 0) sum_parts<LT, false, WEIGHT, TV, false>(r, part_vecs, s0, s1, step, weights_at, apart_at);
-        else sum_parts<LT, false, WEIGHT, TV, true>(r, part_vecs, s0, s1, step, weights_at, apart_at);
+        if (r.lead_a == 0) sum_parts<LT, false, WEIGHT, TV, LONG, false>(r, part_vecs, s0, s1, step, weights_at, apart_at);
+        else sum_parts<LT, false, WEIGHT, TV, LONG, true>(r, part_vecs, s0, s1, step, weights_at, apart_at);
     }
 }
 
@@ -399,7 +412,7 @@ __device__ __forceinline__ int find_token(const PairOfRows<LT> &r, bool pair, Cr
     return tid == 0 ? sh.last : -1;
 }
 
-template <typename LT, bool TV>
+template <typename LT, bool TV, bool LONG>
 __global__ void __launch_bounds__(THREADS, 4) probs_kernel(const ProbsParams p)
 {
     constexpr int VEC = Logit<LT>::VEC;
@@ -505,8 +518,8 @@ __global__ void __launch_bounds__(THREADS, 4) probs_kernel(const ProbsParams p)
 
     const uint32_t weights_at = map_to_rank(smem_addr(sh_weight), 0), apart_at = map_to_rank(smem_addr(sh_apart), 0);
     cluster_wait();
-    if (!TV || n == j) sum_parts<LT, true, TV>(r, pair, part_vecs, s0, s1, WARPS, weights_at, apart_at);
-    else if constexpr (TV) sum_parts<LT, false, true>(r, pair, part_vecs, s0, s1, WARPS, weights_at, apart_at);
+    if (!TV || n == j) sum_parts<LT, true, TV, LONG>(r, pair, part_vecs, s0, s1, WARPS, weights_at, apart_at);
+    else if constexpr (TV) sum_parts<LT, false, true, LONG>(r, pair, part_vecs, s0, s1, WARPS, weights_at, apart_at);
     cluster_sync_all();
     if (rank != 0) return;
 
@@ -577,7 +590,7 @@ __global__ void __launch_bounds__(THREADS, 4) probs_kernel(const ProbsParams p)
         __syncthreads();
         r.certain = -1;
         pair = false;
-        sum_parts<LT, true, TV>(r, false, part_vecs, warp, parts, WARPS, smem_addr(sh_weight), smem_addr(sh_apart));
+        sum_parts<LT, true, TV, LONG>(r, false, part_vecs, warp, parts, WARPS, smem_addr(sh_weight), smem_addr(sh_apart));
         __syncthreads();
     }
     if (TV && n != j) return;
@@ -629,8 +642,12 @@ cudaError_t launch_probs(const ProbsParams &params, int dtype, int n_sm, cudaStr
         cluster = waves(8) <= 1.0 ? 8 : waves(4) <= (lengthy ? n_vec >= 24576 ? 2.75 : 2.1 : 1.0) ? 4 : waves(2) <= (lengthy ? 8.0 : 1.35) ? 2 : 1;
     while (cluster > 1 && p.parts <= WARPS * cluster / 2) cluster /= 2;
     auto launch = [&](auto kernel) { return launch_kernel(kernel, (unsigned)(jobs * cluster), THREADS, 0, cluster, true, stream, p); };
-    if (dtype == METASD_BF16) return p.d_tv ? launch(probs_kernel<__nv_bfloat16, true>) : launch(probs_kernel<__nv_bfloat16, false>);
-    return p.d_tv ? launch(probs_kernel<float, true>) : launch(probs_kernel<float, false>);
+    auto pick = [&](auto plain, auto folding) { return p.part_vecs / 32 * (vec / 2) > CHAIN ? launch(folding) : launch(plain); };
+    if (dtype == METASD_BF16)
+        return p.d_tv ? pick(probs_kernel<__nv_bfloat16, true, false>, probs_kernel<__nv_bfloat16, true, true>)
+                      : pick(probs_kernel<__nv_bfloat16, false, false>, probs_kernel<__nv_bfloat16, false, true>);
+    return p.d_tv ? pick(probs_kernel<float, true, false>, probs_kernel<float, true, true>)
+                  : pick(probs_kernel<float, false, false>, probs_kernel<float, false, true>);
 }
 
 cudaError_t launch_feedback(const VerifyParams &p, const float *d_tv, cudaStream_t stream)

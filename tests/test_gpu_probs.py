@@ -433,3 +433,30 @@ def test_refusals_on_the_device():
     ctx.close()
     with pytest.raises(M.MetasdError):
         ctx.verify_probs(s["target"], s["draft"], s["tokens"], s["u_accept"], s["u_draw"])
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+def test_sums_of_very_long_rows(sign):
+    """Half of the mass ends 2^-32 in front of the end of an entry, or behind it, in a row of 2^24 entries that starts with a large one
+    among small ones: all are multiples of 2^-39 and add up to less than 8, so that sums in fp64 are exact."""
+    V, delta = 1 << 24, sign * 2.0 ** -32
+    w = np.full(V, 2.0 ** -22)
+    w[:104960] = 2.0 ** -24 - 2.0 ** -39
+    w[0] = 1.0
+    upto = np.cumsum(w[:-1])
+    m = int(np.searchsorted(upto, upto[-1] / 2)) + 2
+    w[-1] = 2.0 * (upto[m] - delta) - upto[-1]
+    assert 0.0 < w[-1] <= 2.0 ** -19 and float(np.float32(w[-1])) == w[-1]
+    upto = np.cumsum(w)
+    assert upto[m] - upto[-1] / 2 == delta
+    row = torch.from_numpy(w.astype(np.float32)).to(DEV)
+    u = torch.full((1,), 0.5, device=DEV)
+    want = [m if sign > 0 else m + 1]
+    assert M.verify_probs(row.view(1, 1, V), None, None, None, u).next_token.tolist() == want
+    # the same as what is left over of a row pair, token 3 rejected
+    q = torch.where(torch.arange(V, device=DEV) % 3 == 0, 2.0 ** -20, 0.0)
+    p = row + q
+    assert torch.equal(p.double() - q.double(), row.double())
+    tokens, u_accept = torch.full((1, 1), 3, dtype=torch.int32, device=DEV), torch.full((1, 1), 2.0, device=DEV)
+    out = M.verify_probs(torch.stack([p, row]).view(1, 2, V), q.view(1, 1, V), tokens, u_accept, u)
+    assert out.accepted_len.tolist() == [0] and out.next_token.tolist() == want
