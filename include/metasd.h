@@ -302,9 +302,9 @@ int metasd_verify_noalloc(int32_t batch, int32_t k, int32_t vocab, int32_t logit
  *                        the first rejection n (w = p_n where that leaves nothing), w = p at position k_b if all were accepted
  *   d_tv[b, j]           1/2 sum_v |p_j(v) - q_j(v)|, j < k_b
  *
- * The rows need not be normalised: the accept test takes the values as they are, the draw divides by its own sum (sums of a row stay
- * within the range of fp32; beyond it they count as not finite).  Without d_tv
- * only the drafted tokens' entries and the row (pair) that the next token is drawn from are read.
+ * The rows need not be normalised: the accept test takes the values as they are, the draw divides by its own sum.  Sums (of w, of |p - q|)
+ * above the largest fp32 number count as not finite.  Without d_tv only the drafted tokens' entries and the row (pair) that the next token
+ * is drawn from are read.
  *
  *   ctx            NULL: stateless.  Else the round is one of this context's: batch <= max_batch, 1 <= k <= max_draft, vocab as
  *                  configured; the configured reward (BD: from the d_TV, BE: N_acc / k_b) goes to `reward` and to the bandits, whose

@@ -19,6 +19,7 @@
 // A row is cut into parts by its length alone, a warp sums a part, and the parts' sums are put together in one order:
 // results do not depend on the launch's shape, and the draw re-reads one part (of 80 to 160 of a long row) and not the row.
 #include <algorithm>
+#include <cfloat>
 
 #include "metasd_staged.cuh"
 
@@ -537,7 +538,7 @@ __global__ void __launch_bounds__(THREADS, 4) probs_kernel(const ProbsParams p)
 #pragma unroll
             for (int i = 0; i < PER; ++i) mine += w[i];
             const double upto = lanes_up_to(mine), total = __shfl_sync(FULL, upto, 31);
-            const bool bad = !(total < INFINITY);
+            const bool bad = !(total <= (double)FLT_MAX);
             Crossing x = {0.0, 0.0, 0, 0, 0x7FFFFFFF, -1, false};      // nothing to look for
             if (n == j) {       // the row that the token is drawn from
                 if (total > 0.0 && !bad) {
@@ -576,7 +577,7 @@ __global__ void __launch_bounds__(THREADS, 4) probs_kernel(const ProbsParams p)
                 apart = warp_sum(apart);
                 // a token outside the vocabulary has no place in the row
                 const bool nowhere = !pair && (r.certain < 0 || r.certain >= V);
-                const bool finite = apart < INFINITY;
+                const bool finite = apart <= (double)FLT_MAX;
                 if (!finite) flags |= METASD_STATUS_NONFINITE;
                 if (lane == 0) p.d_tv[(int64_t)b * k + j] = !finite || nowhere ? 1.f : (float)(0.5 * apart);
             }

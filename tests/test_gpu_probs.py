@@ -460,3 +460,24 @@ def test_sums_of_very_long_rows(sign):
     tokens, u_accept = torch.full((1, 1), 3, dtype=torch.int32, device=DEV), torch.full((1, 1), 2.0, device=DEV)
     out = M.verify_probs(torch.stack([p, row]).view(1, 2, V), q.view(1, 1, V), tokens, u_accept, u)
     assert out.accepted_len.tolist() == [0] and out.next_token.tolist() == want
+
+
+@pytest.mark.parametrize("places", [(0, 128), (5, 150000), (7, 199999)])
+def test_sums_beyond_fp32_count_as_not_finite(places):
+    """Wherever in the row the large entries lie: in one lane's sum, in one part's, or in different parts."""
+    V, most = 200000, float(torch.finfo(torch.float32).max)
+    p = torch.full((4, 2, V), 0.25, device=DEV)
+    for b, (x, y) in enumerate([(2.0 ** 127, most - 2.0 ** 127), (2.0 ** 127, 2.0 ** 127), (most, most), (3e38, 1e36)]):
+        p[b, 0] = 0.0
+        p[b, 0, places[0]], p[b, 0, places[1]] = x, y
+    u = torch.zeros(4, device=DEV)
+    word = torch.zeros(1, dtype=torch.int32, device=DEV)
+    out = M.verify_probs(p[:, :1], None, None, None, u, status=word)
+    assert out.next_token.tolist() == [places[0], -1, -1, places[0]] and word.item() == M.STATUS_NONFINITE
+    # distances from a row of zeros
+    tokens, u_accept = torch.full((4, 1), 1, dtype=torch.int32, device=DEV), torch.full((4, 1), 0.5, device=DEV)
+    word.zero_()
+    out = M.verify_probs(p, torch.zeros((4, 1, V), device=DEV), tokens, u_accept, u, want_d_tv=True, status=word)
+    want = 0.5 * np.array([most, 2.0, 2.0, 3.01e38])
+    assert np.all(np.abs(out.d_tv.cpu().numpy()[:, 0] - want) <= TV_RELATIVE * want)
+    assert word.item() == M.STATUS_NONFINITE | M.STATUS_Q_ZERO
