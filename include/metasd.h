@@ -307,7 +307,7 @@ int metasd_verify_noalloc(int32_t batch, int32_t k, int32_t vocab, int32_t logit
  * is drawn from are read.
  *
  *   ctx            NULL: stateless.  Else the round is one of this context's: batch <= max_batch, 1 <= k <= max_draft, vocab as
- *                  configured; the configured reward (BD: from the d_TV, BE: N_acc / k_b) goes to `reward` and to the bandits, whose
+ *                  configured; the configured reward (BD: from the d_TV, those above 1 as 1; BE: N_acc / k_b) goes to `reward` and to the bandits, whose
  *                  next selection metasd_select then returns; status bits go to the context (status is NULL).
  *   device         CUDA device ordinal of the buffers and of `stream`; of the context where there is one
  *   k              0 .. 16; 0: a token is drawn from the target's one row, and what belongs to drafts may be NULL

@@ -600,7 +600,8 @@ __global__ void __launch_bounds__(THREADS, 4) probs_kernel(const ProbsParams p)
 }
 
 // The reward of a round that metasd_verify did not verify, the bandit update and the next selection: a warp per sequence, fp64.  A chain of loads,
-// a logarithm and a square root: 3.2 us behind a round of 64 sequences, 4.1 behind one of 1024.
+// a logarithm and a square root: 3.2 us behind a round of 64 sequences, 4.1 behind one of 1024.  Rows that are not normalised may lie more than 1
+// apart; the policies are made for rewards in [0, 1] (EXP3's weights would all become zeros).
 __global__ void __launch_bounds__(32) feedback_kernel(const VerifyParams p, const float *d_tv)
 {
     __shared__ BanditShared sh;
@@ -608,7 +609,7 @@ __global__ void __launch_bounds__(32) feedback_kernel(const VerifyParams p, cons
     grid_dependency_wait();
     const int b = blockIdx.x, lane = threadIdx.x, k = drafted(p.draft_len, b, p.k);
     const BanditStep step = warp_bandit_fetch(p, b, p.st.t[b], p.st.arm[b], sh);
-    const double align = p.reward_kind == METASD_REWARD_BD && lane < k ? 1.0 - (double)d_tv[(int64_t)b * p.k + lane] : 0.0;
+    const double align = p.reward_kind == METASD_REWARD_BD && lane < k ? 1.0 - fmin((double)d_tv[(int64_t)b * p.k + lane], 1.0) : 0.0;
     const double reward = p.reward_kind == METASD_REWARD_BE ? (double)p.accepted_len[b] / (double)k : warp_sum(align) / (double)k;
     warp_bandit_finish(p, b, step, reward, sh);
     if (lane == 0) p.reward[b] = (float)reward;

@@ -481,3 +481,24 @@ def test_sums_beyond_fp32_count_as_not_finite(places):
     want = 0.5 * np.array([most, 2.0, 2.0, 3.01e38])
     assert np.all(np.abs(out.d_tv.cpu().numpy()[:, 0] - want) <= TV_RELATIVE * want)
     assert word.item() == M.STATUS_NONFINITE | M.STATUS_Q_ZERO
+
+
+@pytest.mark.parametrize("bandit", ["ucb", "ducb", "swucb", "exp3", "petc"])
+def test_rewards_of_rows_that_are_not_normalised(bandit):
+    """Their distances may be above one; the rewards stay in [0, 1], the states finite."""
+    B, K, k, V = 5, 2, 3, 300
+    s = inputs(B, k, V, "fp32", seed=95)
+    s["target"][1:] *= 1e5
+    s["draft"][2:] *= 1e8
+    ctx = M.MetaSD(B, K, k, V, dtype="fp32", bandit=bandit, window=6, gamma=0.3)
+    for _ in range(8):
+        out = ctx.verify_probs(s["target"], s["draft"], s["tokens"], s["u_accept"], s["u_draw"], want_d_tv=True)
+        d_tv = host(out.d_tv)
+        assert (d_tv[0] < 1).all() and (d_tv[1:] > 1e4).all()
+        want = 1.0 - np.minimum(d_tv, 1.0).mean(1)
+        assert np.all(np.abs(host(out.reward) - want) <= 2.0 ** -24) and not host(out.reward)[1:].any()
+    blob = ctx.state_export()
+    state = M.parse_state(blob, B, K, 6)
+    assert np.isfinite(state["stat_a"]).all() and np.isfinite(state["win_reward"]).all()
+    ctx.state_import(blob)
+    ctx.close()
