@@ -600,17 +600,18 @@ template <int THREADS> __global__ void __launch_bounds__(THREADS) release_kernel
             }
             if (n >= MANY) {
                 // Much to give back: the row's warps take a sequence each, and share those that are more than twice a warp's part.
-                auto give = [&](int s, int begin, int by) {
-                    const int d = __shfl_sync(FULL, drop, s), ahead = __shfl_sync(FULL, upto - drop, s), first = __shfl_sync(FULL, from, s);
+                auto give = [&](int s, uint32_t begin, uint32_t by) {      // unsigned: four steps beyond 2^31 - 1 blocks are below 2^32
+                    const uint32_t d = __shfl_sync(FULL, drop, s);
+                    const int ahead = __shfl_sync(FULL, upto - drop, s), first = __shfl_sync(FULL, from, s);
                     const int32_t *source = tables + (int64_t)(row * 32 + s) * c.max_blocks + first;
                     int32_t *to = list + (top - ahead);
-                    for (int e0 = begin; e0 < d; e0 += by * AT_ONCE) {
+                    for (uint32_t e0 = begin; e0 < d; e0 += by * AT_ONCE) {
                         int id[AT_ONCE];
 #pragma unroll
                         for (int i = 0; i < AT_ONCE; ++i) id[i] = e0 + by * i < d ? source[e0 + by * i] : 0;
 #pragma unroll
                         for (int i = 0; i < AT_ONCE; ++i)
-                            if (e0 + by * i < d) to[-(e0 + by * i)] = id[i];
+                            if (e0 + by * i < d) to[-(int64_t)(e0 + by * i)] = id[i];
                     }
                 };
                 unsigned shared = __ballot_sync(FULL, (long long)drop * share > 2ll * n);

@@ -132,6 +132,26 @@ def test_tables_beyond_32_bits():
     assert torch.equal(cache.free_blocks[0], cache.free_blocks[1]) and int(cache.held.sum()) == 0
 
 
+def test_the_longest_table():
+    """One sequence with 2^31 - 1 blocks of one entry: planned, and given back."""
+    n = 2 ** 31 - 1
+    def blocks():
+        return torch.arange(n - 1, -1, -1, dtype=torch.int32, device=DEV)
+    cache = M.BlockCache(torch.full((1, 1, n), -1, dtype=torch.int32, device=DEV), ints([[0]]), blocks().view(1, n), ints([n]), 1)
+    out = M.CachePlan(None, None, None, ints([-7, -7]), torch.full((n,), -7, dtype=torch.int64, device=DEV), None, None)
+    cache.plan(ints([n]), ints([0]), out=out)
+    assert out.token_start.tolist() == [0, n] and cache.held.item() == n and cache.free_count.item() == 0 and cache.last_status() == 0
+    for t in (out.slot_map, cache.block_table[0, 0]):      # the pool hands out 0, 1, 2, ..
+        for at in range(0, n, 2 ** 28):
+            part = t[at:at + 2 ** 28]
+            assert torch.equal(part, torch.arange(at, at + len(part), dtype=t.dtype, device=DEV))
+    del out
+    cache.free_blocks.fill_(-1)
+    cache.release(ints([0]))
+    assert cache.free_count.item() == n and cache.held.item() == 0 and cache.last_status() == 0
+    assert torch.equal(cache.free_blocks[0], blocks())
+
+
 @pytest.mark.parametrize("batch,pools,page,longest", [(3, 2, 1, 5000), (45, 1, 1, 3000), (200, 2, 1, 1500), (700, 1, 2, 700), (70, 3, 3, 3100)])
 def test_releases_of_uneven_tables(batch, pools, page, longest):
     """A few long tables among short and empty ones: a row's blocks given back by one warp each, and by all together."""
