@@ -1,6 +1,8 @@
 """Refusals of metasd_verify_probs, metasd_cache_plan and metasd_cache_release, on the host: before any CUDA call, so that they are
 the same with and without a device; and the plain walks that the GPU tests compare with, on cases worked by hand."""
 import ctypes as C
+import importlib.util
+import os
 from types import SimpleNamespace
 
 import numpy as np
@@ -186,3 +188,44 @@ def test_serving_bookkeeping_where_pools_run_out(seed):
         refs[0].release(in_drafters.tolist())
         refs[1].release(in_target[None].tolist())
     assert went_without > 0
+
+
+@pytest.mark.parametrize("seed", range(8))
+def test_measured_plain_plans_where_pools_run_out(seed):
+    """The plain form that the measured plans are compared with, against the plain walk: nobody behind a sequence that goes without gets blocks,
+    needs none in between or not."""
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "perf", "operators.py")
+    spec = importlib.util.spec_from_file_location("measured_operators", path)
+    operators = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(operators)
+    rng = np.random.default_rng(seed)
+    P, B, page, most, n_blocks = 2, 14, 4, 6, 100
+    cached = rng.integers(0, 3 * page, (P, B))
+    length = cached.max(0) + rng.choice([1, 1, 2, 9], B)
+    pool = rng.integers(-1, P, B)
+    held = -(-cached // page)
+    held += rng.integers(0, 2, (P, B))      # some have a block to spare: they need none
+    ref = Caches(P, B, most, page, [list(range(9 - 4 * g)) for g in range(P)])
+    table = np.full((P, B, most), -1)
+    for g in range(P):
+        for b in range(B):
+            ref.table[g][b] = rng.integers(50, 90, held[g, b]).tolist()
+            table[g, b, :held[g, b]] = ref.table[g][b]
+    free = np.full((P, n_blocks), -1)
+    for g in range(P):
+        free[g, :len(ref.free[g])] = ref.free[g]
+
+    def ints(x):
+        return torch.as_tensor(np.asarray(x), dtype=torch.int32)
+
+    s = dict(table=ints(table), held=ints(held), free=ints(free), count=ints([len(f) for f in ref.free]), cached=ints(cached), length=ints(length),
+             pool=ints(pool), page=page, room=400)
+    got = operators._plain_plan(s)
+    want = ref.plan(length, cached, pool)
+    entries = want[4]
+    assert [g.tolist() for g in got[:4]] == [list(w) for w in want[:4]]
+    for i in range(3):
+        assert got[4 + i][:len(entries)].tolist() == [e[i] for e in entries] and not got[4 + i][len(entries):].any()
+    assert any(e[0] == -1 for e in entries) and any(e[0] >= 0 for e in entries)
+    for g in range(P):
+        assert s["count"][g] == len(ref.free[g]) and [len(t) for t in ref.table[g]] == s["held"][g].tolist()
