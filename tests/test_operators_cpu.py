@@ -199,13 +199,14 @@ def test_measured_plain_plans_where_pools_run_out(seed):
     operators = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(operators)
     rng = np.random.default_rng(seed)
-    P, B, page, most, n_blocks = 2, 14, 4, 6, 100
+    P, B, page, most, n_blocks = 2, 14, 4, 8, 100
     cached = rng.integers(0, 3 * page, (P, B))
     length = cached.max(0) + rng.choice([1, 1, 2, 9], B)
     pool = rng.integers(-1, P, B)
+    pool[2:4], length[2:4] = [0, 1], most * page      # these need four blocks at least, of three and two
     held = -(-cached // page)
     held += rng.integers(0, 2, (P, B))      # some have a block to spare: they need none
-    ref = Caches(P, B, most, page, [list(range(9 - 4 * g)) for g in range(P)])
+    ref = Caches(P, B, most, page, [list(range(3 - g)) for g in range(P)])
     table = np.full((P, B, most), -1)
     for g in range(P):
         for b in range(B):
