@@ -24,8 +24,8 @@
  *     state and its scratch; nothing is allocated after metasd_init.
  *   - Calls are asynchronous on the CUDA stream passed as `stream` (a cudaStream_t, typed void*
  *     so that this header needs no CUDA include); calls on one context must be stream-ordered.
- *     metasd_select, metasd_verify and metasd_reset only launch kernels: they may be captured into
- *     a CUDA graph.  A replay is the context's next round on whatever the captured buffers then
+ *     metasd_select, metasd_verify, metasd_verify_probs, the metasd_cache calls and metasd_reset only launch kernels: they may
+ *     be captured into a CUDA graph.  A replay is the context's next round on whatever the captured buffers then
  *     hold (the round counter that keys the random numbers is device state, not a launch argument).
  *   - The library's kernels are set up while the kernel in front of them in the stream drains and wait for it before they read
  *     anything.  A kernel of the caller's that is itself launched with programmatic stream serialisation must wait for the
@@ -100,7 +100,9 @@ enum metasd_path {
 #define METASD_STATUS_Q_ZERO    4u /* the drafter gave probability 0 to its own drafted token */
 #define METASD_STATUS_TIMEOUT   8u /* a bounded device-side wait on an asynchronous copy ran out (see wait_poll_limit): the
                                       call still ends, its outputs are undefined, the context stays usable */
-#define METASD_STATUS_BAD_LENGTH 32u /* a registered per-sequence draft length was outside 1 .. k: it was clamped */
+#define METASD_STATUS_BAD_LENGTH 32u /* a draft length (registered, or of metasd_verify_probs) was outside 1 .. k, without a context 0 .. k: it was
+                                      clamped; metasd_cache_plan: lengths that do not fit the sequence's table: it adds nothing;
+                                      metasd_cache_release: a negative keep: the sequence gives nothing back in that pool */
 #define METASD_STATUS_BAD_INDEX 64u   /* metasd_verify_probs: a draft_place outside [0, batch); metasd_cache_plan: a pool >= n_pools */
 #define METASD_STATUS_NO_BLOCKS 128u  /* metasd_cache_plan: a pool had too few free blocks; the sequences that went without are
                                          not planned (their slots are -1) */
@@ -307,8 +309,8 @@ int metasd_verify_noalloc(int32_t batch, int32_t k, int32_t vocab, int32_t logit
  * is drawn from are read.
  *
  *   ctx            NULL: stateless.  Else the round is one of this context's: batch <= max_batch, 1 <= k <= max_draft, vocab as
- *                  configured; the configured reward (BD: from the d_TV, those above 1 as 1; BE: N_acc / k_b) goes to `reward` and to the bandits, whose
- *                  next selection metasd_select then returns; status bits go to the context (status is NULL).
+ *                  configured; the configured reward (BD: from the d_TV, those above 1 as 1; BE: N_acc / k_b) goes to `reward` and to the bandits,
+ *                  whose next selection metasd_select then returns; status bits go to the context (status is NULL).
  *   device         CUDA device ordinal of the buffers and of `stream`; of the context where there is one
  *   k              0 .. 16; 0: a token is drawn from the target's one row, and what belongs to drafts may be NULL
  *   vocab          V, up to 2^30
@@ -331,7 +333,7 @@ int metasd_verify_noalloc(int32_t batch, int32_t k, int32_t vocab, int32_t logit
  * Defined outcomes: an entry of a drafted token that is NaN, infinite or negative rejects it, a row that holds such an entry has
  * d_TV 1 and gives token -1, as a row of zeros does (METASD_STATUS_NONFINITE); a drafted token outside the vocabulary is
  * rejected; a certain drafter's distance to such a token is 1; q(x) = 0 < p(x) is accepted.
- * Launches kernels only (one; with a context two): may be captured.  Results are the same, bit for bit, in a batch of any size. */
+ * Outputs overlap no input.  Launches kernels only (one; with a context two): may be captured.  Results are the same, bit for bit, in a batch of any size. */
 int metasd_verify_probs(metasd_ctx *ctx, int32_t device, int32_t batch, int32_t k, int32_t vocab, int32_t prob_dtype,
                         const void *target_probs, int64_t target_seq_stride, int64_t target_row_stride,
                         const void *draft_probs, int64_t draft_seq_stride, int64_t draft_row_stride,
@@ -377,7 +379,8 @@ size_t metasd_cache_workspace_bytes(int32_t max_batch, int32_t n_pools);   /* 0:
  * Blocks are taken from the end of the pool's free list, sequence after sequence in that order; from the first sequence on for
  * which too few are left, none of the pool gets any (those that need none are planned).  Behind token_start[batch] the
  * outputs are left as they were.  A sequence whose lengths do not fit its table (METASD_STATUS_BAD_LENGTH) or whose pool does not
- * exist (METASD_STATUS_BAD_INDEX) adds nothing.  Launches kernels only; calls on one cache must be stream-ordered. */
+ * exist (METASD_STATUS_BAD_INDEX) adds nothing.  Outputs overlap no input.  Launches kernels only; calls on one cache must be
+ * stream-ordered. */
 int metasd_cache_plan(const metasd_cache *cache, int32_t batch, const int32_t *pool, const int32_t *cached,
                       int64_t cached_pool_stride, const int32_t *length, int32_t max_tokens, int32_t *order,
                       int32_t *place, int32_t *pool_start, int32_t *token_start, int64_t *slot_map,
@@ -385,7 +388,9 @@ int metasd_cache_plan(const metasd_cache *cache, int32_t batch, const int32_t *p
 
 /* Gives back the blocks that sequences b < batch hold beyond keep entries (rejected drafts, finished queries), in every pool:
  * keep[g * keep_pool_stride + b] entries stay (0: nothing; more than are held: all).  The free list grows so that the next plan
- * takes the blocks in the order (sequence, then position) in which they were held: a release undoes a plan. */
+ * takes the blocks in the order (sequence, then position) in which they were held: a release undoes a plan.  Where keep is negative
+ * nothing comes back (METASD_STATUS_BAD_LENGTH); a pool to whose list more would come back than it has room for gets none and its
+ * tables stay as they are (METASD_STATUS_BAD_STATE). */
 int metasd_cache_release(const metasd_cache *cache, int32_t batch, const int32_t *keep, int64_t keep_pool_stride, void *stream);
 
 const char *metasd_strerror(int code);

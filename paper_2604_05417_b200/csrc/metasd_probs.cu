@@ -13,9 +13,9 @@
 // to an edge.  Chains and lanes join in fp64.
 //
 // Bound by memory: without distances one row pair per sequence is read (the one that the token is drawn from), with them every
-// pair.  512 sequences of 152064 fp32 entries without: 93 us, 6.6 TB/s; 256 x 7 pairs of 128256 bf16 entries with: 148 us, 6.3 TB/s
+// pair.  512 sequences of 152064 fp32 entries without: 94 us, 6.5 TB/s; 256 x 7 pairs of 128256 bf16 entries with: 149 us, 6.2 TB/s
 // (a copy makes 6.5).  Small calls are a chain: the accept tests' two dependent loads 1.0 us, a part 1.1, the blocks' meeting 0.6, the
-// parts' sums and the draw 1.5; one sequence of 32000 entries 4.9 us.
+// parts' sums and the draw 1.5; one sequence of 32000 entries 5.1 us.
 // A row is cut into parts by its length alone, a warp sums a part, and the parts' sums are put together in one order:
 // results do not depend on the launch's shape, and the draw re-reads one part (of 80 to 160 of a long row) and not the row.
 #include <algorithm>
@@ -635,6 +635,8 @@ cudaError_t launch_probs(const ProbsParams &params, int dtype, int n_sm, cudaStr
     //     1792: 154.0, 152.9, 168.0
     //   V = 50264 with distances, rows 120: 26.8, 18.3, 14.7, 15.8; 300: 32.7, 31.7, 28.7, 32.7; 640: 57.4, 49.0, 50.3, 65.3
     //   V = 32000, bf16, rows 100: 9.4, 8.9, 8.1, 10.1; 300: 16.2, 13.9, 15.6, 23.6; 600: 21.8, 23.8, 28.7; 1000: 30.7, 35.7, 44.6
+    // The rule is a simple one and not the table's best everywhere: V = 128256 with distances, rows 448 (0.76 of a wave) take 1; V = 152064, rows 440
+    // (0.74) take 2; V = 50264 with distances, rows 500 (0.84) take 1: 41.4 where 2 take 38.8.  0.55: lengths spread evenly over 0 .. k.
     const double rows = !p.d_tv ? p.batch : p.draft_len ? 0.55 * p.batch * (p.k + 1) : (double)p.batch * p.k;
     const auto waves = [&](int blocks) { return rows * blocks / (4.0 * n_sm); };
     const bool lengthy = n_vec >= 8192;     // 128 KB

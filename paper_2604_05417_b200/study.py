@@ -229,8 +229,9 @@ def serving_rounds(wl: Workload, rounds: int, bandit: str, device=0, seed: int =
 
 def serving_run(wl: Workload, rounds: int, bandit: str, **options) -> dict:
     """serving_rounds, summed up: entries that the drafters' and the target's caches add per sequence and round (k - 1 drafts
-    and k + 1 tokens if nobody fell behind and all was accepted), the share of rounds in which a drafter had to catch up with more than
-    the last round, blocks held per sequence, the best-arm ratio and the block efficiency."""
+    and k + 1 tokens if nobody fell behind and all was accepted), the share of sequences and rounds whose drafter
+    had more than k + 1 tokens to catch up with (the first use of every drafter on a query, by its prompt, is among them; a drafter that missed one
+    short round is not), blocks held per sequence, the best-arm ratio and the block efficiency."""
     entries_d = entries_t = behind = held = acc = best = 0.0
     status = 0
     for r in serving_rounds(wl, rounds, bandit, **options):
